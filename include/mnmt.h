@@ -335,6 +335,125 @@ int mnmt_logits_argmax_noalloc(const int8_t* d_X, const int8_t* d_Wp, const floa
 int mnmt_fold_requant(float s_in, const float* h_s_w, const float* h_b, float s_out, int N,
                       float* h_scale, float* h_bias);
 
+/* ---- paged key/value cache -------------------------------------------------- */
+
+/* A pool of pages that hold the int8 key and value codes of `page_size` tokens
+ * each, per layer, and tables that say which pages a row (a hypothesis, a
+ * sequence) has.  The pool, the tables and the lengths are the caller's device
+ * memory; the pages are used by every layer alike, so one table serves all.
+ *
+ * Pool, int8: [n_layers][n_pages], of each page first the keys
+ * [n_kv_heads][page_size][d_head], then the values in groups of 16 tokens,
+ * [n_kv_heads][page_size / 16][d_head][16] (the order in which the attention
+ * kernel's matrix operand wants them).  n_layers * n_pages * page bytes in all
+ * (mnmt_pages_bytes).
+ * Table, int32 [rows][max_pages]: token t of a row lies in page
+ * table[row][t / page_size] at t % page_size.  -1, and any number outside
+ * 0..n_pages-1, means that there is no page: keys there are skipped, codes
+ * written there are dropped.  Lengths, int32 [rows], in tokens (values outside
+ * 0..max_pages * page_size count as the nearest of these).  Rows may share
+ * pages.  A page that no row's table names within its length is free; nothing
+ * else is kept, so a caller frees rows by leaving them out. */
+typedef struct {
+  int32_t n_layers;   /* 1..256 */
+  int32_t n_pages;    /* pages of a layer, 1..2^22 */
+  int32_t page_size;  /* tokens: 16, 32, 64, 128 or 256 */
+  int32_t n_kv_heads; /* 1..256 */
+  int32_t d_head;     /* a multiple of 16, 16..128 */
+  int32_t max_pages;  /* pages of a row (the table's row stride); max_pages * page_size <= 2^30 */
+} mnmt_pages_cfg;
+
+/* Bytes of the pool, and of the workspace of a fork or compaction of `rows`
+ * output rows; 0 where the arguments are refused.  Host only. */
+size_t mnmt_pages_bytes(const mnmt_pages_cfg* cfg);
+size_t mnmt_pages_ws_bytes(const mnmt_pages_cfg* cfg, int rows);
+
+/* The tables of the next step: output row r goes on from input row d_parent[r]
+ * (int32 [rows]; any number outside 0..rows_in-1: the row is empty; NULL: row r
+ * itself), with room for d_new[r] more tokens (int32 [rows]; a negative number
+ * drops the last tokens; NULL: 0).  d_len_out[r] is the length with them.
+ * Several rows may have one parent.  They share its pages, except that a page
+ * which a row is to write to (its last one, where d_new[r] > 0 and the kept
+ * tokens end inside it) belongs to that row alone: the lowest such row keeps it
+ * if no row shares it, the others get copies, of all layers.  Copies and new
+ * pages are taken from the free pages in ascending order, by the rows in
+ * order.  Pages that only dropped rows had are free.
+ * d_info int32 [2]: free pages left, pages missing.  Where pages are missing
+ * (or a length would exceed the table: it stops there) the entries that got none
+ * are -1, and nothing has been copied: the input tables still hold, and the call
+ * can be made again with fewer rows.
+ * The outputs may not overlap the inputs, except that without d_parent they may
+ * be the input table and lengths themselves. */
+int mnmt_pages_fork(const mnmt_pages_cfg* cfg, void* d_pool, const int32_t* d_table, const int32_t* d_len, int rows_in,
+                    const int32_t* d_parent, const int32_t* d_new, int rows, int32_t* d_table_out, int32_t* d_len_out,
+                    int32_t* d_info, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Move the pages that the rows use to the numbers 0..live-1: those below stay,
+ * the k-th above goes to the k-th free one below, in every layer.  d_table_out
+ * (which may be d_table) names the new places, -1 past each row's length.
+ * d_info int32 [2]: live pages, pages moved. */
+int mnmt_pages_compact(const mnmt_pages_cfg* cfg, void* d_pool, const int32_t* d_table, const int32_t* d_len, int rows,
+                       int32_t* d_table_out, int32_t* d_info, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Write the keys and values of new tokens into a layer's pages.  d_k, d_v int8:
+ * token i's codes [n_kv_heads][d_head] at d_k + i * ld, d_v + i * ld (bytes, a
+ * multiple of 16; K and V may lie side by side in one linear layer's output).
+ * Row r has the tokens d_start[r]..d_start[r+1]-1 (int32 [rows + 1]; NULL: n /
+ * rows each); they are its last ones, so its lengths count them already
+ * (mnmt_pages_fork) and token i of m goes to position d_len[r] - m + i; those at
+ * negative positions are dropped.  max_q: the most tokens of a row, as far as
+ * the caller knows it (it sizes the launch; larger rows are written too). */
+int mnmt_pages_write(const mnmt_pages_cfg* cfg, void* d_pool, int layer, const int32_t* d_table, const int32_t* d_len,
+                     int rows, const int8_t* d_k, const int8_t* d_v, int64_t ld, const int32_t* d_start, int n,
+                     int max_q, void* stream);
+
+/* ---- attention ---------------------------------------------------------------- */
+
+/* out[t][h] = c_pv sum_j p_j v_j / sum_j p_j, p_j = exp(c_qk (q . k_j) - max), over
+ * the keys j that query t sees; 0 where it sees none.  Queries, keys and values
+ * are int8 codes; query head h reads key head h / (n_heads / n_kv_heads).
+ *   MNMT_ATTN_I8:  int8 clamp(rint(.), -127, 127), c_pv = s_v / s_out
+ *   MNMT_ATTN_F32: fp32, c_pv = s_v
+ * c_qk = s_q s_k / sqrt(d_head).  Scores and sums of products are exact
+ * integers; a weight p is held to 2^-21 of the largest.  A call's results do not
+ * change from run to run; they may differ in the last bits between launch plans
+ * (max_q, max_len) and from a session's, whose fp32 order is the canonical one. */
+#define MNMT_ATTN_I8 0
+#define MNMT_ATTN_F32 1
+
+typedef struct {
+  int32_t n_heads; /* query heads: a multiple of n_kv_heads, at most 4096 */
+  int32_t kind;    /* MNMT_ATTN_* */
+  int32_t causal;  /* mnmt_attn_paged: token i of a row's m sees its positions 0..len - m + i; else 0..len - 1 */
+  int32_t ld_q;    /* row stride of the queries, bytes: a multiple of 16, >= n_heads * d_head */
+  int32_t ld_out;  /* row stride of the output, elements: a multiple of 4, >= n_heads * d_head */
+  int32_t max_q;   /* the most queries of a row and the longest length, as far as the caller knows them: */
+  int32_t max_len; /*   they plan the launch, larger ones are computed too */
+  float c_qk, c_pv;
+} mnmt_attn_cfg;
+
+/* Workspace of an attention call (0: none is needed).  Host only. */
+size_t mnmt_attn_ws_bytes(int rows, int n_heads, int n_kv_heads, int d_head, int max_q, int max_len);
+
+/* Attention of a chunk of new tokens of each row over the pages of a layer; a
+ * decoding step is a chunk of one token.  d_q int8 [n][ld_q], heads side by
+ * side; row r has the tokens d_start[r]..d_start[r+1]-1 (int32 [rows + 1]; NULL:
+ * n / rows each), its last ones: their keys are in the cache already.  d_out
+ * [n][ld_out]; outputs of tokens that no row has are left as they are. */
+int mnmt_attn_paged(const mnmt_pages_cfg* pages, const mnmt_attn_cfg* cfg, const void* d_pool, int layer,
+                    const int32_t* d_table, const int32_t* d_len, int rows, const int8_t* d_q, const int32_t* d_start,
+                    int n, void* d_out, void* d_ws, size_t ws_bytes, void* stream);
+
+/* Attention to an encoder's keys and values: row b (a source sentence) has d_len[b]
+ * of them (0..S), key j at d_k + b * batch + j * ld, value j at d_v + ..., int8
+ * [n_kv_heads][d_head]; ld and batch in bytes, multiples of 16 (the session
+ * tensor "cross_kv.<l>" is such a pair side by side).  Its queries, of all its
+ * hypotheses and their tokens, are d_start[b]..d_start[b+1]-1 (NULL: n / rows
+ * each) of d_q; all see every key (causal must be 0). */
+int mnmt_attn_cross(const mnmt_attn_cfg* cfg, int n_kv_heads, int d_head, const int8_t* d_k, const int8_t* d_v,
+                    int64_t ld, int64_t batch, int S, const int32_t* d_len, int rows, const int8_t* d_q,
+                    const int32_t* d_start, int n, void* d_out, void* d_ws, size_t ws_bytes, void* stream);
+
 /* ---- canonical arithmetic self-check -------------------------------------- */
 
 /* Run the engine's device fp32 primitives on d_x[n] -> d_y[n]: fn 0 exp

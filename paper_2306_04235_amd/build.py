@@ -25,7 +25,7 @@ DEVICE = [f"--offload-arch={ARCH}", "-fno-gpu-flush-denormals-to-zero", "-fhip-f
 # per-file device flags: the GEMM keeps its matrix-core accumulators in VGPRs
 EXTRA = {"gemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
 SOURCES = ["qlinear.hip", "kernels.hip", "decode_fused.hip", "decode_step.hip", "decode_rows.hip", "encode_rows.hip", "encode_small.hip", "gemm.hip", "logits.hip",
-           "noalloc.hip", "model.cpp", "session.cpp", "api.cpp"]
+           "noalloc.hip", "pages.hip", "attn_paged.hip", "attn_cross.hip", "model.cpp", "session.cpp", "api.cpp", "cache.cpp"]
 
 
 def _compile(src: str, verbose: bool) -> str:

@@ -23,6 +23,16 @@ __device__ __forceinline__ v4i mfma16(const v4i a, const v4i b, const v4i c) {
   return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
 }
 
+// 4 x 4 bytes: byte b of x[i] becomes byte i of the b-th result.
+__device__ __forceinline__ void transpose4(const uint32_t* x, uint32_t& y0, uint32_t& y1, uint32_t& y2, uint32_t& y3) {
+  const uint32_t a = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), b = __builtin_amdgcn_perm(x[1], x[0], 0x07030602u);
+  const uint32_t c = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u), d = __builtin_amdgcn_perm(x[3], x[2], 0x07030602u);
+  y0 = __builtin_amdgcn_perm(c, a, 0x05040100u);
+  y1 = __builtin_amdgcn_perm(c, a, 0x07060302u);
+  y2 = __builtin_amdgcn_perm(d, b, 0x05040100u);
+  y3 = __builtin_amdgcn_perm(d, b, 0x07060302u);
+}
+
 // 4-bit weight codes (the paper's W-E-A 4-8-8 setting) widened to int8: in
 // each group of 16 codes of a row, packed byte i (i < 8) holds code i in its
 // low nibble and code i + 8 in its high nibble, each plus 8.  Per byte,

@@ -19,10 +19,14 @@ OK, E_INVALID_ARG, E_BAD_MODEL, E_CAPACITY, E_HIP, E_UNSUPPORTED, E_TIMEOUT = 0,
 
 LOAD_PACKED_4BIT_ONLY = 1
 
+ATTN_I8, ATTN_F32 = 0, 1
+
 EXPORTS = ("mnmt_model_bytes", "mnmt_model_load", "mnmt_model_bytes_ex", "mnmt_model_load_ex", "mnmt_model_get_info", "mnmt_model_free", "mnmt_session_bytes",
            "mnmt_session_create", "mnmt_session_free", "mnmt_encode", "mnmt_decode_step", "mnmt_translate",
            "mnmt_session_status", "mnmt_session_tensor", "mnmt_qlinear", "mnmt_qlinear_w4", "mnmt_qlinear_timed",
            "mnmt_argmax_partials", "mnmt_packed_bytes", "mnmt_pack_weights", "mnmt_logits_argmax_noalloc",
+           "mnmt_pages_bytes", "mnmt_pages_ws_bytes", "mnmt_pages_fork", "mnmt_pages_compact", "mnmt_pages_write",
+           "mnmt_attn_ws_bytes", "mnmt_attn_paged", "mnmt_attn_cross",
            "mnmt_fold_requant", "mnmt_debug_canon", "mnmt_debug_read", "mnmt_status_str", "mnmt_last_error")
 
 
@@ -47,6 +51,15 @@ class SessionCfg(C.Structure):
 class SearchCfg(C.Structure):
     _fields_ = [("beam", C.c_int32), ("max_steps", C.c_int32), ("len_penalty_alpha", C.c_float),
                 ("stop_at_eos", C.c_int32), ("use_graph", C.c_int32)]
+
+
+class PagesCfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_layers", "n_pages", "page_size", "n_kv_heads", "d_head", "max_pages")]
+
+
+class AttnCfg(C.Structure):
+    _fields_ = [(n, C.c_int32) for n in ("n_heads", "kind", "causal", "ld_q", "ld_out", "max_q", "max_len")] + [
+        ("c_qk", C.c_float), ("c_pv", C.c_float)]
 
 
 _lib = None
@@ -88,6 +101,18 @@ def lib():
         L.mnmt_debug_canon.argtypes = [i32, vp, i32, vp, vp]
         L.mnmt_debug_read.argtypes = [vp, sz, i32, vp, vp]
         L.mnmt_logits_argmax_noalloc.argtypes = [vp, vp, vp, i32, i32, i32, vp, vp, vp]
+        i64, pages, attn = C.c_int64, C.POINTER(PagesCfg), C.POINTER(AttnCfg)
+        L.mnmt_pages_bytes.argtypes = [pages]
+        L.mnmt_pages_bytes.restype = sz
+        L.mnmt_pages_ws_bytes.argtypes = [pages, i32]
+        L.mnmt_pages_ws_bytes.restype = sz
+        L.mnmt_pages_fork.argtypes = [pages, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp, sz, vp]
+        L.mnmt_pages_compact.argtypes = [pages, vp, vp, vp, i32, vp, vp, vp, sz, vp]
+        L.mnmt_pages_write.argtypes = [pages, vp, i32, vp, vp, i32, vp, vp, i64, vp, i32, i32, vp]
+        L.mnmt_attn_ws_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+        L.mnmt_attn_ws_bytes.restype = sz
+        L.mnmt_attn_paged.argtypes = [pages, attn, vp, i32, vp, vp, i32, vp, vp, i32, vp, vp, sz, vp]
+        L.mnmt_attn_cross.argtypes = [attn, i32, i32, vp, vp, i64, i64, i32, vp, i32, vp, vp, i32, vp, vp, sz, vp]
         L.mnmt_status_str.argtypes = [i32]
         L.mnmt_status_str.restype = C.c_char_p
         L.mnmt_last_error.argtypes = []
@@ -275,6 +300,216 @@ def mnmt_debug_read(x, sink, reps=1, stream=None):
         raise ValueError("sink needs 2048 32-bit words")
     _check(lib().mnmt_debug_read(_ptr(x), x.numel() * x.element_size(), int(reps), _ptr(sink), _stream(stream)),
            "mnmt_debug_read")
+
+
+# ---- paged cache and attention ---------------------------------------------------------
+def pages_cfg(pool, max_pages: int) -> PagesCfg:
+    """The configuration of a pool int8 [n_layers, n_pages, 2, n_kv_heads, page_size, d_head]: of a page's two halves
+    the first holds the keys in that order, the second the values as [n_kv_heads, page_size / 16, d_head, 16]."""
+    L, n, two, hkv, P, dh = pool.shape
+    _need(two == 2 and pool.dtype == _torch().int8 and pool.is_contiguous(),
+          "the pool must be a contiguous int8 tensor [n_layers, n_pages, 2, n_kv_heads, page_size, d_head]")
+    return PagesCfg(L, n, P, hkv, dh, max_pages)
+
+
+_torch_module = None
+
+
+def _torch():
+    global _torch_module
+    if _torch_module is None:
+        import torch
+
+        _torch_module = torch
+    return _torch_module
+
+
+def _need(ok, what):
+    if not ok:
+        raise ValueError(what)
+
+
+def _ints(name, t, shape, like):
+    """Checks an int32 tensor that the kernels read as a dense array."""
+    _need(t.dtype == _torch().int32 and tuple(t.shape) == shape and t.is_contiguous() and t.device == like.device,
+          f"{name} must be a contiguous int32 tensor {list(shape)} on {like.device}")
+
+
+def _codes(name, t, width, like):
+    """Checks int8 rows [n, width] whose columns are adjacent; their stride."""
+    _need(t.dtype == _torch().int8 and t.dim() == 2 and t.shape[1] == width and t.device == like.device
+          and (t.numel() == 0 or t.stride(1) == 1), f"{name} must be int8 [n, {width}] on {like.device}, its columns adjacent")
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+class _on:
+    """Makes the tensors' device the current one for a call (its stream and its launches belong there)."""
+
+    def __init__(self, t):
+        _need(t.is_cuda, f"the tensors must be on a GPU, not on {t.device}")
+        self.index = t.device.index
+
+    def __enter__(self):
+        cuda = _torch().cuda
+        self.before = cuda.current_device()
+        if self.before != self.index:
+            cuda.set_device(self.index)
+
+    def __exit__(self, *_):
+        if self.before != self.index:
+            _torch().cuda.set_device(self.before)
+
+
+def _workspace(nbytes, like, stream):
+    """A call's own workspace, so that calls on different streams and captured graphs never share one."""
+    if nbytes == 0:
+        return None
+    t = _torch().empty(nbytes, dtype=_torch().uint8, device=like.device)
+    if stream is not None:
+        t.record_stream(stream)  # (the allocator would give it to the current stream's next call)
+    return t
+
+
+def mnmt_pages_fork(pool, table, lens, parent=None, new=None, out=None, stream=None):
+    """The next step's tables: row r goes on from row parent[r] (outside the table: empty; None: itself) with room for
+    new[r] more tokens.  Returns (table int32 [rows, max_pages], lengths int32 [rows], info int32 [2]: free pages left,
+    pages missing); out: these three tensors."""
+    torch = _torch()
+    rows_in, width = table.shape
+    rows = rows_in if parent is None else parent.shape[0]
+    cfg = pages_cfg(pool, width)
+    _ints("table", table, (rows_in, width), pool)
+    _ints("lens", lens, (rows_in,), pool)
+    if parent is not None:
+        _ints("parent", parent, (rows,), pool)
+    if new is not None:
+        _ints("new", new, (rows,), pool)
+    with _on(pool):
+        if out is None:
+            out = (torch.empty((rows, width), dtype=torch.int32, device=pool.device),
+                   torch.empty(rows, dtype=torch.int32, device=pool.device),
+                   torch.empty(2, dtype=torch.int32, device=pool.device))
+        else:
+            for name, t, shape in zip(("out[0]", "out[1]", "out[2]"), out, ((rows, width), (rows,), (2,))):
+                _ints(name, t, shape, pool)
+        ws = _workspace(lib().mnmt_pages_ws_bytes(C.byref(cfg), rows), pool, stream)
+        rc = lib().mnmt_pages_fork(C.byref(cfg), _ptr(pool), _ptr(table), _ptr(lens), rows_in, _ptr(parent), _ptr(new),
+                                   rows, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(ws),
+                                   0 if ws is None else ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "mnmt_pages_fork")
+    return out
+
+
+def mnmt_pages_compact(pool, table, lens, out=None, stream=None):
+    """Moves the pages in use to the lowest numbers.  Returns (table int32 [rows, max_pages], info int32 [2]: live pages,
+    pages moved); out: these two tensors (out[0] may be the table itself)."""
+    torch = _torch()
+    rows, width = table.shape
+    cfg = pages_cfg(pool, width)
+    _ints("table", table, (rows, width), pool)
+    _ints("lens", lens, (rows,), pool)
+    with _on(pool):
+        if out is None:
+            out = (torch.empty((rows, width), dtype=torch.int32, device=pool.device),
+                   torch.empty(2, dtype=torch.int32, device=pool.device))
+        else:
+            _ints("out[0]", out[0], (rows, width), pool)
+            _ints("out[1]", out[1], (2,), pool)
+        ws = _workspace(lib().mnmt_pages_ws_bytes(C.byref(cfg), rows), pool, stream)
+        rc = lib().mnmt_pages_compact(C.byref(cfg), _ptr(pool), _ptr(table), _ptr(lens), rows, _ptr(out[0]),
+                                      _ptr(out[1]), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "mnmt_pages_compact")
+    return out
+
+
+def mnmt_pages_write(pool, layer, table, lens, k, v, start=None, max_q=None, stream=None):
+    """Writes the codes k, v int8 [n, n_kv_heads * d_head] of new tokens, the last ones of their rows, into a layer's
+    pages; row r has the tokens start[r] .. start[r + 1] - 1 (None: n / rows each), at most max_q as far as known."""
+    rows, width = table.shape
+    cfg = pages_cfg(pool, width)
+    _ints("table", table, (rows, width), pool)
+    _ints("lens", lens, (rows,), pool)
+    ld = _codes("k", k, cfg.n_kv_heads * cfg.d_head, pool)
+    n = k.shape[0]
+    _need(_codes("v", v, k.shape[1], pool) == ld and v.shape[0] == n, "k and v must have the same rows and row stride")
+    if start is not None:
+        _ints("start", start, (rows + 1,), pool)
+    with _on(pool):
+        rc = lib().mnmt_pages_write(C.byref(cfg), _ptr(pool), layer, _ptr(table), _ptr(lens), rows, _ptr(k), _ptr(v), ld,
+                                    _ptr(start), n, n if max_q is None else max_q, _stream(stream))
+    if rc:
+        _check(rc, "mnmt_pages_write")
+
+
+def _attn_out(q, kind, out):
+    torch = _torch()
+    dt = torch.int8 if kind == ATTN_I8 else torch.float32
+    if out is None:
+        return torch.empty(tuple(q.shape), dtype=dt, device=q.device)
+    _need(out.dtype == dt and out.shape == q.shape and out.device == q.device and (out.numel() == 0 or out.stride(1) == 1),
+          f"out must be {dt} {list(q.shape)} on {q.device}, its columns adjacent")
+    return out
+
+
+def mnmt_attn_paged(q, pool, layer, table, lens, c_qk, c_pv, kind=ATTN_F32, start=None, causal=True, max_q=None,
+                    max_len=None, out=None, stream=None):
+    """Attention of the rows' last tokens, q int8 [n, n_heads * d_head], over a layer's pages: fp32 or (ATTN_I8) int8 of
+    q's shape.  Row r has the tokens start[r] .. start[r + 1] - 1 (None: n / rows each); max_q and max_len: the most of
+    a row and the longest length, as far as known."""
+    rows, width = table.shape
+    cfg = pages_cfg(pool, width)
+    _ints("table", table, (rows, width), pool)
+    _ints("lens", lens, (rows,), pool)
+    n, d = q.shape
+    _need(d > 0 and d % cfg.d_head == 0, "q must have whole heads")
+    ld = _codes("q", q, d, pool)
+    if start is not None:
+        _ints("start", start, (rows + 1,), pool)
+    with _on(pool):
+        out = _attn_out(q, kind, out)
+        most = n // max(rows, 1) if start is None else n if max_q is None else min(n, max_q)
+        longest = width * cfg.page_size if max_len is None else min(max_len, width * cfg.page_size)
+        a = AttnCfg(d // cfg.d_head, kind, int(causal), ld, out.stride(0) if n > 1 else d, most,
+                    longest, c_qk, c_pv)
+        ws = _workspace(lib().mnmt_attn_ws_bytes(rows, a.n_heads, cfg.n_kv_heads, cfg.d_head, most, longest), pool, stream)
+        rc = lib().mnmt_attn_paged(C.byref(cfg), C.byref(a), _ptr(pool), layer, _ptr(table), _ptr(lens), rows, _ptr(q),
+                                   _ptr(start), n, _ptr(out), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "mnmt_attn_paged")
+    return out
+
+
+def mnmt_attn_cross(q, k, v, lens, d_head, c_qk, c_pv, kind=ATTN_F32, start=None, max_q=None, out=None, stream=None):
+    """Attention of q int8 [n, n_heads * d_head] to the keys and values int8 [rows, S, n_kv_heads * d_head] of each
+    query's source sentence, lens[b] of them: fp32 or (ATTN_I8) int8 of q's shape.  Sentence b has the queries
+    start[b] .. start[b + 1] - 1 (None: n / rows each), at most max_q as far as known."""
+    torch = _torch()
+    rows, S, width = k.shape
+    n, d = q.shape
+    _need(d_head > 0 and d % d_head == 0 and width % d_head == 0 and d > 0 and width > 0, "q, k and v must have whole heads")
+    for name, t in (("k", k), ("v", v)):
+        _need(t.dtype == torch.int8 and t.shape == k.shape and t.device == q.device
+              and (t.numel() == 0 or (t.stride() == k.stride() and t.stride(2) == 1)),
+              f"{name} must be int8 [rows, S, n_kv_heads * d_head] on {q.device}, its columns adjacent, k and v strided alike")
+    _ints("lens", lens, (rows,), q)
+    ldq = _codes("q", q, d, q)
+    if start is not None:
+        _ints("start", start, (rows + 1,), q)
+    hkv = width // d_head
+    ld = k.stride(1) if S > 1 else width
+    with _on(q):
+        out = _attn_out(q, kind, out)
+        most = n // max(rows, 1) if start is None else n if max_q is None else min(n, max_q)
+        a = AttnCfg(d // d_head, kind, 0, ldq, out.stride(0) if n > 1 else d, most, S, c_qk, c_pv)
+        ws = _workspace(lib().mnmt_attn_ws_bytes(rows, a.n_heads, hkv, d_head, most, S), q, stream)
+        rc = lib().mnmt_attn_cross(C.byref(a), hkv, d_head, _ptr(k), _ptr(v), ld, k.stride(0) if rows > 1 else 0, S,
+                                   _ptr(lens), rows, _ptr(q), _ptr(start), n, _ptr(out), _ptr(ws),
+                                   0 if ws is None else ws.numel(), _stream(stream))
+    if rc:
+        _check(rc, "mnmt_attn_cross")
+    return out
 
 
 class Model:

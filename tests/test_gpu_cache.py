@@ -1,0 +1,587 @@
+"""The paged cache and the attention operators on the GPU against the plain
+forms of cache_ref.py: whole numbers exactly, attention within a derived bound
+of float64."""
+import numpy as np
+import pytest
+
+from . import cache_ref as R
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def gpu():
+    import torch
+
+    from paper_2306_04235_amd import mnmt
+
+    assert torch.cuda.is_available(), "GPU tests need a visible GPU"
+    return torch, mnmt
+
+
+def dev(torch, a, dtype=None):
+    a = np.ascontiguousarray(a)
+    return torch.from_numpy(a if dtype is None else a.astype(dtype)).cuda()
+
+
+def codes(rng, *shape):
+    return np.clip(np.rint(rng.normal(0, 32, shape)), -127, 127).astype(np.int8)
+
+
+def make(rng, L, n_pages, hkv, P, dh, lens, width=None, share=0):
+    """A random pool and a table of distinct pages; the first `share` pages of all rows are row 0's."""
+    count = [-(-max(int(x), 0) // P) for x in lens]
+    width = width or max(1, max(count))
+    ids = rng.permutation(n_pages)
+    table, at = np.full((len(lens), width), -1, np.int32), 0
+    for r, c in enumerate(count):
+        for i in range(min(c, width)):
+            if r and i < share and i < count[0]:
+                table[r, i] = table[0, i]
+            else:
+                table[r, i], at = ids[at], at + 1
+    return codes(rng, L, n_pages, 2, hkv, P, dh), table
+
+
+def starts(new):
+    return np.concatenate([[0], np.cumsum(new)]).astype(np.int32)
+
+
+# ---- attention over pages -------------------------------------------------------------
+def run_paged(gpu, seed, lens, new, h, hkv, dh, P, kind="f32", causal=True, c_qk=None, c_pv=1 / 32, width=None,
+              hints=None, table_edit=None, share=0, edit=None, layers=1, layer=0, strided=True):
+    torch, mnmt = gpu
+    rng = np.random.default_rng(seed)
+    lens, new = np.asarray(lens), np.asarray(new)
+    pages = sum(-(-max(int(x), 0) // P) for x in lens) + 3
+    pool, table = make(rng, layers, pages, hkv, P, dh, lens, width, share)
+    if table_edit:
+        table_edit(table)
+    n = int(new.sum())
+    q = codes(rng, n, h * dh)
+    if edit:
+        edit(q, pool, rng)
+    c_qk = 1.5 / (1024 * dh ** 0.5) if c_qk is None else c_qk
+    qd = dev(torch, q)
+    if strided:  # the first columns of a wider row
+        wide = torch.full((n, (h + 2 * hkv) * dh), 99, dtype=torch.int8, device="cuda")
+        wide[:, : h * dh] = qd
+        qd = wide[:, : h * dh]
+    start = None if len(set(new.tolist())) == 1 else dev(torch, starts(new))
+    got = mnmt.mnmt_attn_paged(qd, dev(torch, pool), layer, dev(torch, table), dev(torch, lens, np.int32), c_qk, c_pv,
+                               kind=mnmt.ATTN_I8 if kind == "i8" else mnmt.ATTN_F32, start=start, causal=causal,
+                               **(hints or {})).cpu().numpy()
+    ref, tol = R.paged(R.Cache(pool), layer, table, lens, q, starts(new), h, np.float32(c_qk), np.float32(c_pv), causal)
+    if kind == "i8":
+        R.check_codes(got, ref, tol)
+    else:
+        assert (np.abs(got - ref) <= tol).all()
+        norm = np.linalg.norm(ref)
+        assert np.linalg.norm(got - ref) <= 1e-5 * norm + 1e-30
+    return got
+
+
+@pytest.mark.parametrize("dh", [16, 32, 48, 64, 80, 96, 112, 128])
+@pytest.mark.parametrize("P", [16, 64])
+def test_step_over_head_widths(gpu, dh, P):
+    """One token per row, lengths at the edges of groups, tiles and pages."""
+    run_paged(gpu, dh + P, [1, 2, 15, 16, 17, 63, 64, 65, 127, 128, 129, 200], [1] * 12, 4, 4, dh, P)
+
+
+@pytest.mark.parametrize("dh", [16, 48, 64, 128])
+@pytest.mark.parametrize("P", [32, 128, 256])
+@pytest.mark.parametrize("h, hkv", [(2, 2), (7, 1), (6, 3), (32, 2)])
+def test_chunks_over_head_layouts(gpu, dh, P, h, hkv):
+    run_paged(gpu, dh + P + h, [5, 70, 131, 64, 33], [5, 17, 40, 1, 0], h, hkv, dh, P)
+
+
+@pytest.mark.parametrize("kind", ["f32", "i8"])
+@pytest.mark.parametrize("causal", [True, False])
+def test_ragged_chunks(gpu, kind, causal):
+    run_paged(gpu, 3, [300, 1, 77, 500, 64], [130, 1, 60, 3, 64], 8, 4, 64, 16, kind, causal, c_pv=3.0 if kind == "i8" else 0.5)
+
+
+@pytest.mark.parametrize("kind", ["f32", "i8"])
+def test_empty_rows_and_queries_before_the_start(gpu, kind):
+    """Rows of length 0 and below, lengths past the table, tokens at negative positions: zeros or what is there."""
+    got = run_paged(gpu, 4, [0, 3, -5, 40, 1000], [2, 5, 2, 2, 2], 4, 2, 32, 16, kind, width=4)
+    assert not got[:2].any() and not got[2:4].any() and not got[7:9].any() and got[9:].any()
+
+
+def test_missing_pages(gpu):
+    """Entries that name no page (also far outside) hide their keys."""
+    def edit(table):
+        table[0, 1], table[1, 0], table[2, :], table[3, 2] = -1, 1 << 30, -7, -(1 << 31)
+    got = run_paged(gpu, 5, [40, 30, 33, 300], [1, 30, 4, 1], 4, 2, 64, 16, table_edit=edit)
+    assert not got[31:35].any()
+
+
+def test_shared_pages(gpu):
+    run_paged(gpu, 6, [100, 90, 70], [4, 4, 4], 8, 8, 64, 16, share=4)
+
+
+@pytest.mark.parametrize("c_qk", [0.0, 1e-30, 1e-6, 0.02, 1.0, 1e6, 1e30])
+def test_scales_of_the_scores(gpu, c_qk):
+    """From plain means to one key that takes all; ties of the largest score share it."""
+    run_paged(gpu, 7, [200, 65], [1, 30], 4, 2, 64, 32, c_qk=c_qk)
+
+
+@pytest.mark.parametrize("new", [1, 40])
+def test_growing_scores(gpu, new):
+    """Each key scores higher than those before, so that the reference has to move all the time; and falling ones."""
+    def grow(sign):
+        def edit(q, pool, rng):
+            q[:] = 100
+            t = np.arange(pool.shape[4])
+            pool[:, :, 0] = np.clip(sign * (t[None, None, None, :, None] - 128), -127, 127)
+        return edit
+    for sign in (1, -1):
+        run_paged(gpu, 8, [256], [new], 2, 2, 64, 256, c_qk=3e-4, edit=grow(sign))
+
+
+def test_extreme_codes(gpu):
+    def edit(q, pool, rng):
+        q[:] = rng.choice([-128, 127], q.shape)
+        pool[:] = rng.choice([-128, 127], pool.shape)
+    run_paged(gpu, 9, [130, 64], [3, 3], 4, 1, 128, 16, c_qk=2e-5, c_pv=1.0, edit=edit)
+
+
+@pytest.mark.parametrize("rows, lens, h, hkv, dh", [(1, [5000], 8, 8, 64), (2, [3000, 129], 16, 2, 128), (1, [40000], 2, 1, 32),
+                                                     (3, [255, 4097, 1], 4, 4, 80)])
+@pytest.mark.parametrize("kind", ["f32", "i8"])
+def test_long_rows(gpu, rows, lens, h, hkv, dh, kind):
+    """Few rows and many keys: ranges of the keys in different blocks, joined."""
+    run_paged(gpu, 10 + rows, lens, [1] * rows, h, hkv, dh, 64, kind, c_pv=12.0 if kind == "i8" else 1 / 32)
+
+
+def test_long_chunk_over_few_rows(gpu):
+    run_paged(gpu, 14, [2000, 1024], [40, 24], 4, 2, 64, 32)
+
+
+def test_more_keys_than_one_fold(gpu):
+    """A wave folds its integer sums after 65,536 keys: one query tile over 140,000, with weights that hardly differ."""
+    run_paged(gpu, 15, [140000], [1], 1, 1, 16, 256, c_qk=1e-5, hints=dict(max_len=100))
+
+
+@pytest.mark.parametrize("hints", [dict(max_q=1, max_len=1), dict(max_q=3, max_len=300), dict(max_q=1000, max_len=1 << 20)])
+def test_bounds_are_hints(gpu, hints):
+    """Rows beyond max_q and max_len are computed all the same."""
+    run_paged(gpu, 16, [900, 1500, 30], [70, 200, 1], 4, 2, 64, 16, hints=hints)
+    run_paged(gpu, 17, [9000], [1], 4, 2, 64, 16, hints=dict(max_len=hints["max_len"]))
+
+
+def test_layers_and_dense_queries(gpu):
+    run_paged(gpu, 18, [50, 20], [3, 3], 4, 4, 64, 16, layers=3, layer=2, strided=False)
+
+
+def test_many_rows(gpu):
+    rng = np.random.default_rng(19)
+    run_paged(gpu, 19, rng.integers(1, 100, 700), [1] * 700, 8, 8, 64, 16)
+
+
+def test_tokens_of_no_row_are_left(gpu):
+    """Outputs behind the last row, between rows and beside the heads' columns stay as they were."""
+    torch, mnmt = gpu
+    rng = np.random.default_rng(20)
+    lens = np.array([40, 17], np.int32)
+    pool, table = make(rng, 1, 9, 2, 16, 64, lens)
+    q = codes(rng, 12, 256)
+    out = torch.full((12, 260), 7.0, device="cuda")
+    start = np.array([2, 5, 9], np.int32)
+    mnmt.mnmt_attn_paged(dev(torch, q), dev(torch, pool), 0, dev(torch, table), dev(torch, lens), 1e-4, 1.0,
+                         start=dev(torch, start), out=out[:, :256])
+    out = out.cpu().numpy()
+    ref, tol = R.paged(R.Cache(pool), 0, table, lens, q, start, 4, np.float32(1e-4), 1.0)
+    assert (out[:2] == 7).all() and (out[9:] == 7).all() and (out[:, 256:] == 7).all()
+    assert (np.abs(out[2:9, :256] - ref[2:9]) <= tol[2:9]).all()
+
+
+def test_starts_out_of_range(gpu):
+    """Starts outside 0..n, and falling ones, count as the nearest that make sense."""
+    torch, mnmt = gpu
+    rng = np.random.default_rng(21)
+    lens = np.array([30, 30, 30], np.int32)
+    pool, table = make(rng, 1, 9, 2, 16, 32, lens)
+    q = codes(rng, 6, 64)
+    out = torch.full((6, 64), 7.0, device="cuda")
+    mnmt.mnmt_attn_paged(dev(torch, q), dev(torch, pool), 0, dev(torch, table), dev(torch, lens), 1e-4, 1.0,
+                         start=dev(torch, np.array([-5, 2, 1, 1 << 30], np.int32)), out=out)
+    ref, tol = R.paged(R.Cache(pool), 0, table[[0, 2]], lens[:2], np.concatenate([q[:2], q[1:]]),
+                       np.array([0, 2, 7]), 2, np.float32(1e-4), 1.0)
+    got = out.cpu().numpy()
+    assert (np.abs(got[0] - ref[0]) <= tol[0]).all()
+    assert (np.abs(got[2:] - ref[3:]) <= tol[3:]).all()  # (token 1 belongs to both: either's result)
+
+
+def test_pool_past_4_gib(gpu):
+    """Pages whose offsets do not fit 32 bits, read and written."""
+    torch, mnmt = gpu
+    hkv, P, dh, n_pages = 8, 256, 128, 10000  # 512 KiB a page
+    pool = torch.zeros((1, n_pages, 2, hkv, P, dh), dtype=torch.int8, device="cuda")
+    rng = np.random.default_rng(22)
+    table, lens = np.array([[n_pages - 1, 2], [5, 9000]], np.int32), np.array([300, 400], np.int32)
+    k, v = codes(rng, 700, hkv * dh), codes(rng, 700, hkv * dh)
+    start = starts([300, 400])
+    mnmt.mnmt_pages_write(pool, 0, dev(torch, table), dev(torch, lens), dev(torch, k), dev(torch, v), start=dev(torch, start))
+    small = np.array([[0, 1], [2, 3]], np.int32)
+    ids = torch.from_numpy(table.reshape(-1).astype(np.int64)).cuda()
+    ref = R.Cache(np.zeros((1, 4, 2, hkv, P, dh), np.int8))
+    ref.write(0, small, lens, k, v, start)
+    assert np.array_equal(pool[:, ids].cpu().numpy(), ref.pool())
+    assert int((pool.view(n_pages, -1).amax(1) != 0).sum()) == 4
+    q = codes(rng, 2, 8 * dh)
+    got = mnmt.mnmt_attn_paged(dev(torch, q), pool, 0, dev(torch, table), dev(torch, lens), 1e-4, 0.5).cpu().numpy()
+    want, tol = R.paged(ref, 0, small, lens, q, starts([1, 1]), 8, np.float32(1e-4), 0.5)
+    assert (np.abs(got - want) <= tol).all()
+
+
+# ---- cross attention ------------------------------------------------------------------
+def run_cross(gpu, seed, lens, new, h, hkv, dh, S, kind="f32", c_pv=1 / 32, c_qk=None, form="pair", hints=None):
+    torch, mnmt = gpu
+    rng = np.random.default_rng(seed)
+    lens, new = np.asarray(lens), np.asarray(new)
+    n, B = int(new.sum()), len(lens)
+    q, kv = codes(rng, n, h * dh), codes(rng, B, S, 2, hkv * dh)
+    c_qk = 1.5 / (1024 * dh ** 0.5) if c_qk is None else c_qk
+    k, v = dev(torch, kv[:, :, 0]), dev(torch, kv[:, :, 1])
+    if form == "pair":  # side by side, as a linear layer leaves them
+        both = dev(torch, kv.reshape(B, S, -1))
+        k, v = both[..., : hkv * dh], both[..., hkv * dh:]
+    elif form == "late":  # time before batch
+        k, v = (a.transpose(0, 1).contiguous().transpose(0, 1) for a in (k, v))
+    start = None if len(set(new.tolist())) == 1 else dev(torch, starts(new))
+    got = mnmt.mnmt_attn_cross(dev(torch, q), k, v, dev(torch, lens, np.int32), dh, c_qk, c_pv,
+                               kind=mnmt.ATTN_I8 if kind == "i8" else mnmt.ATTN_F32, start=start,
+                               **(hints or {})).cpu().numpy()
+    ref, tol = np.zeros((n, h * dh)), np.zeros((n, h, dh))
+    at = starts(new)
+    for b in range(B):
+        length = min(max(int(lens[b]), 0), S)
+        x, tol[at[b]: at[b + 1]] = R.attend(q[at[b]: at[b + 1]].reshape(-1, h, dh), kv[b, :length, 0].reshape(length, hkv, dh),
+                                            kv[b, :length, 1].reshape(length, hkv, dh), np.ones((int(new[b]), length), bool),
+                                            np.float32(c_qk), c_pv)
+        ref[at[b]: at[b + 1]] = x.reshape(-1, h * dh)
+    tol = tol.reshape(n, -1)
+    if kind == "i8":
+        R.check_codes(got, ref, tol)
+    else:
+        assert (np.abs(got - ref) <= tol).all()
+        assert np.linalg.norm(got - ref) <= 1e-5 * np.linalg.norm(ref) + 1e-30
+    return got
+
+
+@pytest.mark.parametrize("dh", [16, 32, 48, 64, 80, 96, 112, 128])
+@pytest.mark.parametrize("form", ["pair", "apart", "late"])
+def test_cross_over_head_widths(gpu, dh, form):
+    run_cross(gpu, dh, [1, 2, 15, 16, 17, 63, 64, 65, 90], [4] * 9, 4, 4, dh, 90, form=form)
+
+
+@pytest.mark.parametrize("h, hkv", [(1, 1), (6, 6), (7, 1), (24, 8)])
+@pytest.mark.parametrize("kind", ["f32", "i8"])
+def test_cross_ragged(gpu, h, hkv, kind):
+    run_cross(gpu, h, [100, 0, 7, -3, 128, 1000], [1, 3, 0, 2, 50, 17], h, hkv, 64, 131, kind, c_pv=6.0 if kind == "i8" else 1.0)
+
+
+@pytest.mark.parametrize("S", [1, 5, 700, 3001])
+def test_cross_lengths(gpu, S):
+    run_cross(gpu, S, [S, max(S // 2, 1)], [3, 3], 8, 4, 64, S)
+    run_cross(gpu, S, [S], [1], 2, 1, 128, S, form="late", hints=dict(max_q=1))
+
+
+def test_cross_chunk(gpu):
+    run_cross(gpu, 30, [400, 333, 90], [150, 200, 1], 8, 8, 64, 400, hints=dict(max_q=5))
+
+
+def test_cross_no_source(gpu):
+    assert not run_cross(gpu, 31, [0, 0], [2, 2], 4, 4, 32, 0, form="apart").any()
+
+
+# ---- pages -----------------------------------------------------------------------------
+def forked(gpu, cache_pool, table, lens, parent, new, rows=None, in_place=False):
+    torch, mnmt = gpu
+    pool, t, l = dev(torch, cache_pool), dev(torch, table), dev(torch, lens, np.int32)
+    opt = {k: None if a is None else dev(torch, a, np.int32) for k, a in (("parent", parent), ("new", new))}
+    out = (t, l, torch.empty(2, dtype=torch.int32, device="cuda")) if in_place else None
+    got = mnmt.mnmt_pages_fork(pool, t, l, out=out, **opt)
+    ref = R.Cache(cache_pool)
+    want = ref.fork(table, lens, parent, new)
+    for a, b in zip(got, want):
+        assert np.array_equal(a.cpu().numpy(), b)
+    assert np.array_equal(pool.cpu().numpy(), ref.pool())
+    return [a.cpu().numpy() for a in got], pool.cpu().numpy()
+
+
+@pytest.mark.parametrize("seed", range(12))
+def test_fork_random(gpu, seed):
+    rng = np.random.default_rng(100 + seed)
+    P, hkv, dh, L = [(16, 2, 16, 1), (32, 1, 48, 3), (16, 4, 64, 2), (64, 3, 128, 2)][seed % 4]
+    rows_in, rows = int(rng.integers(1, 40)), int(rng.integers(1, 60))
+    lens = rng.integers(0, 5 * P, rows_in)
+    pool, table = make(rng, L, 5 * rows_in + 2 * rows + 8, hkv, P, dh, lens, width=7, share=int(rng.integers(0, 3)))
+    parent = rng.integers(-1, rows_in + 1, rows)
+    new = rng.integers(-20, 40, rows) if seed % 2 else np.ones(rows, int)
+    forked(gpu, pool, table, lens, parent, new)
+
+
+@pytest.mark.parametrize("rows, width, n_pages", [(1, 1, 1), (1500, 3, 9000), (70, 300, 40000), (5000, 2, 20000)])
+def test_fork_sizes(gpu, rows, width, n_pages):
+    rng = np.random.default_rng(rows)
+    lens = rng.integers(0, width * 16, rows)
+    pool, table = make(rng, 1, n_pages, 1, 16, 16, lens, width=width)
+    forked(gpu, pool, table, lens, rng.integers(0, rows, rows), np.ones(rows, int))
+
+
+def test_fork_identity_and_in_place(gpu):
+    rng = np.random.default_rng(3)
+    lens = rng.integers(0, 60, 9)
+    pool, table = make(rng, 2, 60, 2, 16, 32, lens, width=6)
+    for in_place in (False, True):
+        forked(gpu, pool, table, lens, None, rng.integers(0, 30, 9), in_place=in_place)
+        forked(gpu, pool, table, lens, None, None, in_place=in_place)
+
+
+def test_fork_of_shared_last_pages(gpu):
+    """Rows that share a page which they are to write to: also where one of them only reads, or has it in its middle."""
+    rng = np.random.default_rng(4)
+    pool = codes(rng, 1, 12, 2, 1, 16, 16)
+    table = np.array([[3, 4, -1], [3, 4, 5], [4, 3, -1], [3, 4, -1]], np.int32)
+    lens = np.array([20, 40, 24, 20])
+    for new in ([1, 1, 1, 1], [0, 1, 1, 0], [1, 0, 0, 1], [1, -30, -9, 1], [-4, -40, -8, -4]):
+        forked(gpu, pool, table, lens, None, np.array(new))
+        forked(gpu, pool, table, lens, np.array([3, 2, 1, 0]), np.array(new))
+
+
+def test_fork_out_of_pages(gpu):
+    """Too few free pages: -1 entries in the last rows, the count of what is missing, and no page changed."""
+    rng = np.random.default_rng(5)
+    lens = np.array([20, 20, 33])
+    pool, table = make(rng, 2, 9, 2, 16, 32, lens, width=4)
+    (t, l, info), after = forked(gpu, pool, table, lens, np.array([0, 0, 1, 1, 2, 2, 2]), np.full(7, 20))
+    assert info[0] == 0 and info[1] > 0 and np.array_equal(after, pool)
+    (t, l, info), after = forked(gpu, pool, table, lens, np.array([0, 1]), np.full(2, 20))
+    assert info[1] == 0
+
+
+def test_fork_lengths_and_entries_out_of_range(gpu):
+    rng = np.random.default_rng(6)
+    lens = np.array([-4, 1 << 30, 50, 40])
+    pool, table = make(rng, 1, 30, 1, 16, 16, [0, 64, 50, 40], width=4)
+    table[2, 1], table[2, 3], table[3, 2] = 1 << 29, -9, 77
+    forked(gpu, pool, table, lens, np.array([0, 1, 2, 3, 2, 9, -(1 << 31)]), np.array([5, 3, 1, 1, 1, 2, 0]))
+    forked(gpu, pool, table, lens, np.array([0, 1, 2, 3]), np.array([(1 << 31) - 1, -(1 << 31), 2, 2]))
+
+
+def test_fork_to_no_rows(gpu):
+    torch, mnmt = gpu
+    pool = torch.zeros((1, 7, 2, 1, 16, 16), dtype=torch.int8, device="cuda")
+    table, lens = torch.zeros((2, 1), dtype=torch.int32, device="cuda"), torch.ones(2, dtype=torch.int32, device="cuda")
+    none = torch.empty(0, dtype=torch.int32, device="cuda")
+    t, l, info = mnmt.mnmt_pages_fork(pool, table, lens, parent=none)
+    assert t.shape == (0, 1) and l.shape == (0,) and info.tolist() == [7, 0]
+    t, info = mnmt.mnmt_pages_compact(pool, table[:0], lens[:0])
+    assert info.tolist() == [0, 0]
+
+
+@pytest.mark.parametrize("seed", range(8))
+def test_compact_random(gpu, seed):
+    torch, mnmt = gpu
+    rng = np.random.default_rng(200 + seed)
+    P, hkv, dh, L = [(16, 2, 16, 1), (32, 1, 48, 3), (16, 4, 64, 2), (64, 3, 128, 2)][seed % 4]
+    rows = int(rng.integers(1, 50))
+    lens = rng.integers(-3, 5 * P, rows)
+    n_pages = [5 * rows, 5 * rows + 3000][seed // 4]
+    pool, table = make(rng, L, n_pages, hkv, P, dh, lens, width=6, share=int(rng.integers(0, 3)))
+    if seed % 2:
+        table[0, 0] = n_pages + 5
+    for in_place in (False, True):
+        p, t = dev(torch, pool), dev(torch, table)
+        out = (t, torch.empty(2, dtype=torch.int32, device="cuda")) if in_place else None
+        got = mnmt.mnmt_pages_compact(p, t, dev(torch, lens, np.int32), out=out)
+        ref = R.Cache(pool)
+        want = ref.compact(table, lens)
+        assert np.array_equal(got[0].cpu().numpy(), want[0]) and np.array_equal(got[1].cpu().numpy(), want[1])
+        assert np.array_equal(p.cpu().numpy(), ref.pool())
+
+
+@pytest.mark.parametrize("P, hkv, dh", [(16, 4, 64), (32, 1, 16), (64, 3, 80), (256, 2, 128)])
+@pytest.mark.parametrize("ragged", [True, False])
+def test_write(gpu, P, hkv, dh, ragged):
+    """Chunks that begin and end inside groups, whole groups, empty rows, missing pages, tokens before the start."""
+    torch, mnmt = gpu
+    rng = np.random.default_rng(P + ragged)
+    lens = np.array([1, 16, 17, 40, 300, 5, 64, 0, 33, 90])
+    new = np.array([1, 16, 3, 40, 200, 9, 16, 4, 0, 35]) if ragged else np.full(10, 7)
+    pool, table = make(rng, 2, 100, hkv, P, dh, lens, width=-(-280 // P))
+    table[9, 0], table[6, 0] = -1, 500
+    n = int(new.sum())
+    both = codes(rng, n + 2, 3 * hkv * dh)
+    pd, bd = dev(torch, pool), dev(torch, both)
+    ref = R.Cache(pool)
+    start = starts(new) + ragged  # (the first row of k and v belongs to nobody)
+    k, v = (bd[: n + 2 * ragged, (1 + i) * hkv * dh: (2 + i) * hkv * dh] for i in (0, 1))
+    for hint in (None, 1) if ragged else (None,):
+        mnmt.mnmt_pages_write(pd, 1, dev(torch, table), dev(torch, lens, np.int32), k, v,
+                              start=dev(torch, start, np.int32) if ragged else None, max_q=hint)
+        ref.write(1, table, lens, both[:, hkv * dh: 2 * hkv * dh], both[:, 2 * hkv * dh:], start)
+        assert np.array_equal(pd.cpu().numpy(), ref.pool())
+        pd.copy_(dev(torch, pool))
+
+
+# ---- together --------------------------------------------------------------------------
+def test_beam_search_steps_of_a_decoder_layer(gpu):
+    """The operators as a decoder layer uses them: Q/K/V of a step's tokens from a quantized linear layer, forked tables,
+    codes written, self-attention over the pages, its output layer, cross attention over the encoder's keys and values.
+    Every context against float64 over the hypotheses' own histories, kept without pages."""
+    torch, mnmt = gpu
+    rng = np.random.default_rng(50)
+    B, W, d, h, dh, P, steps, S = 5, 4, 256, 4, 64, 16, 40, 37
+    rows = B * W
+    wq = dev(torch, codes(rng, 3 * d, d))
+    scale = dev(torch, np.full(3 * d, 1 / (32 * 16.0), np.float32))
+    bias = dev(torch, rng.normal(0, 4, 3 * d).astype(np.float32))
+    kv, slen = codes(rng, B, S, 2 * d), np.array([S, 1, 20, 16, 33])
+    kvd, slen_d = dev(torch, kv), dev(torch, slen, np.int32)
+    pool = torch.zeros((1, 3 * rows + 2 * rows, 2, h, P, dh), dtype=torch.int8, device="cuda")
+    table = torch.full((rows, 3), -1, dtype=torch.int32, device="cuda")
+    lens = torch.zeros(rows, dtype=torch.int32, device="cuda")
+    one = torch.ones(rows, dtype=torch.int32, device="cuda")
+    past = [([], []) for _ in range(rows)]
+    c_qk, c_pv, c_x = np.float32(1e-4), np.float32(3.0), np.float32(1 / 32)
+    for step in range(steps):
+        parent = (rng.integers(0, W, (B, W)) + W * np.arange(B)[:, None]).reshape(-1)
+        table, lens, info = mnmt.mnmt_pages_fork(pool, table, lens, parent=dev(torch, parent, np.int32), new=one)
+        assert info[1].item() == 0 and lens.eq(step + 1).all()
+        x = dev(torch, codes(rng, rows, d))
+        qkv = mnmt.mnmt_qlinear(x, wq, scale, bias, mnmt.EPI_I8)
+        mnmt.mnmt_pages_write(pool, 0, table, lens, qkv[:, d: 2 * d], qkv[:, 2 * d:])
+        ctx = mnmt.mnmt_attn_paged(qkv[:, :d], pool, 0, table, lens, c_qk, c_pv, kind=mnmt.ATTN_I8)
+        y = mnmt.mnmt_qlinear(ctx, wq[:d], scale[:d], bias[:d], mnmt.EPI_I8)
+        z = mnmt.mnmt_attn_cross(y, kvd[..., :d], kvd[..., d:], slen_d, dh, c_qk, c_x)
+        a, y, z = qkv.cpu().numpy(), y.cpu().numpy(), z.cpu().numpy()
+        past = [(past[p][0] + [a[r, d: 2 * d]], past[p][1] + [a[r, 2 * d:]]) for r, p in enumerate(parent)]
+        both = [R.attend(a[r: r + 1, :d].reshape(1, h, dh), np.stack(past[r][0]).reshape(-1, h, dh),
+                         np.stack(past[r][1]).reshape(-1, h, dh), np.ones((1, step + 1), bool), c_qk, c_pv) for r in range(rows)]
+        ref, tol = (np.concatenate([np.broadcast_to(x[i], (1, h, dh)) for x in both]).reshape(rows, d) for i in (0, 1))
+        R.check_codes(ctx.cpu().numpy(), ref, tol)
+        for r in range(0, rows, 7):
+            n = slen[r // W]
+            want, tol = R.attend(y[r: r + 1].reshape(1, h, dh), kv[r // W, :n, :d].reshape(n, h, dh),
+                                 kv[r // W, :n, d:].reshape(n, h, dh), np.ones((1, n), bool), c_qk, c_x)
+            assert (np.abs(z[r].reshape(1, h, dh) - want) <= tol).all()
+        if step % 13 == 12:
+            table, info = mnmt.mnmt_pages_compact(pool, table, lens)
+            assert info[0].item() == len(set(t for t in table.cpu().numpy().reshape(-1).tolist() if t >= 0))
+    # then two more tokens each as one chunk, checked against the steps' keys and values
+    table, lens, _ = mnmt.mnmt_pages_fork(pool, table, lens, new=2 * one)
+    qkv = mnmt.mnmt_qlinear(dev(torch, codes(rng, 2 * rows, d)), wq, scale, bias, mnmt.EPI_I8)
+    mnmt.mnmt_pages_write(pool, 0, table, lens, qkv[:, d: 2 * d], qkv[:, 2 * d:])
+    got = mnmt.mnmt_attn_paged(qkv[:, :d], pool, 0, table, lens, c_qk, c_x).cpu().numpy()
+    a = qkv.cpu().numpy()
+    for r in range(rows):
+        k = np.stack(past[r][0] + [a[2 * r, d: 2 * d], a[2 * r + 1, d: 2 * d]]).reshape(-1, h, dh)
+        v = np.stack(past[r][1] + [a[2 * r, 2 * d:], a[2 * r + 1, 2 * d:]]).reshape(-1, h, dh)
+        seen = np.arange(steps + 2)[None, :] <= steps + np.arange(2)[:, None]
+        want, tol = R.attend(a[2 * r: 2 * r + 2, :d].reshape(2, h, dh), k, v, seen, c_qk, c_x)
+        assert (np.abs(got[2 * r: 2 * r + 2].reshape(2, h, dh) - want) <= tol).all()
+
+
+def test_cross_attention_over_a_sessions_keys(gpu):
+    """The session's cross-attention keys and values of a decoder layer are such a pair."""
+    torch, mnmt = gpu
+    from synth import generate as G
+
+    model = mnmt.Model(G.build_model(G.TINY))
+    d, h = model.info.d_model, model.info.n_heads
+    src, lens = G.make_sources(1000, 3, [5, 9, 2], seed=3, s_max=9)
+    sess = mnmt.Session(model, 3, 9, 4)
+    sess.encode(torch.from_numpy(src).cuda(), torch.from_numpy(lens).cuda())
+    kv = sess.tensor("cross_kv.0", torch.int8, (3, 9, 2 * d))
+    rng = np.random.default_rng(1)
+    q = codes(rng, 6, d)
+    got = mnmt.mnmt_attn_cross(dev(torch, q), kv[..., :d], kv[..., d:], torch.from_numpy(lens).cuda(), d // h, 1e-3, 0.25)
+    got, kv = got.cpu().numpy(), kv.cpu().numpy()
+    for b in range(3):
+        n = int(lens[b])
+        want, tol = R.attend(q[2 * b: 2 * b + 2].reshape(2, h, d // h), kv[b, :n, :d].reshape(n, h, d // h),
+                             kv[b, :n, d:].reshape(n, h, d // h), np.ones((2, n), bool), np.float32(1e-3), 0.25)
+        assert (np.abs(got[2 * b: 2 * b + 2].reshape(2, h, d // h) - want) <= tol).all()
+    sess.close()
+    model.close()
+
+
+def step_of(gpu, seed, rows=6, length=700):
+    """A step of all operators as a closure over fixed buffers, and what it leaves."""
+    torch, mnmt = gpu
+    rng = np.random.default_rng(seed)
+    h, dh, P = 4, 64, 16
+    lens = np.full(rows, length)
+    pool, table = make(rng, 2, 60 * rows, h, P, dh, lens, width=60)
+    pd, td, ld = dev(torch, pool), dev(torch, table), dev(torch, lens, np.int32)
+    qkv = dev(torch, codes(rng, rows, 3 * h * dh))
+    kv = dev(torch, codes(rng, rows, 600, 2 * h * dh))
+    slen = dev(torch, rng.integers(1, 600, rows), np.int32)
+    parent, one = dev(torch, rng.integers(0, rows, rows), np.int32), torch.ones(rows, dtype=torch.int32, device="cuda")
+    d = h * dh
+
+    def step(stream=None):
+        t, l, info = mnmt.mnmt_pages_fork(pd, td, ld, parent=parent, new=one, stream=stream)
+        mnmt.mnmt_pages_write(pd, 1, t, l, qkv[:, d: 2 * d], qkv[:, 2 * d:], stream=stream)
+        a = mnmt.mnmt_attn_paged(qkv[:, :d], pd, 1, t, l, 1e-4, 0.5, stream=stream)
+        x = mnmt.mnmt_attn_cross(qkv[:, :d], kv[..., :d], kv[..., d:], slen, dh, 1e-4, 0.5, stream=stream)
+        return t, l, info, a, x
+
+    return step, qkv, pd
+
+
+def test_captured_and_replayed(gpu):
+    """Two captured steps, replayed by turns and at once with eager ones between: each replay as the eager run of its inputs."""
+    torch, _ = gpu
+    steps, graphs = [step_of(gpu, s) for s in (60, 61)], []
+    for step, _, _ in steps:
+        side = torch.cuda.Stream()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            step()
+        torch.cuda.current_stream().wait_stream(side)
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = step()
+        graphs.append((g, out))
+    rng = np.random.default_rng(62)
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    for round_ in range(4):
+        want = []
+        for step, qkv, pool in steps:
+            qkv.copy_(dev(torch, codes(rng, *qkv.shape)))
+            want.append(([x.clone() for x in step()], pool.clone()))
+        torch.cuda.synchronize()
+        if round_ % 2:
+            for (g, _), s in zip(graphs, streams):
+                with torch.cuda.stream(s):
+                    g.replay()
+        else:
+            for g, _ in graphs:
+                g.replay()
+        torch.cuda.synchronize()
+        for (_, out), (step, _, pool), (w, p) in zip(graphs, steps, want):
+            for a, b in zip(out, w):
+                assert torch.equal(a, b)
+            assert torch.equal(pool, p)
+
+
+def test_streams(gpu):
+    """Steps on two streams at once, given as an argument and as the current one, repeat the default stream's results."""
+    torch, _ = gpu
+    steps = [step_of(gpu, s, rows=3, length=900) for s in (70, 71)]
+    want = [[x.clone() for x in step()] for step, _, _ in steps]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream(), torch.cuda.Stream()]
+    got = [[], []]
+    for _ in range(5):
+        got[0].append(steps[0][0](stream=streams[0]))
+        with torch.cuda.stream(streams[1]):
+            got[1].append(steps[1][0]())
+    torch.cuda.synchronize()
+    for outs, w in zip(got, want):
+        for o in outs:
+            assert all(torch.equal(a, b) for a, b in zip(o, w))
