@@ -415,7 +415,7 @@ int mnmt_pages_write(const mnmt_pages_cfg* cfg, void* d_pool, int layer, const i
  *   MNMT_ATTN_I8:  int8 clamp(rint(.), -127, 127), c_pv = s_v / s_out
  *   MNMT_ATTN_F32: fp32, c_pv = s_v
  * c_qk = s_q s_k / sqrt(d_head).  Scores and sums of products are exact
- * integers; a weight p is held to 2^-21 of the largest.  A call's results do not
+ * integers; a weight p is held to 2^-24 of the largest.  A call's results do not
  * change from run to run; they may differ in the last bits between launch plans
  * (max_q, max_len) and from a session's, whose fp32 order is the canonical one. */
 #define MNMT_ATTN_I8 0

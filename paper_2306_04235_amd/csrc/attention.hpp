@@ -16,14 +16,13 @@
 // products with exact int32 sums, joined as 65536 a + 256 b + c.  Adding 2^23 +
 // 0x8080 to the scaled p rounds it and leaves the digits in the bytes of the
 // float (0x8080 makes the lower digits signed once their top bits are flipped).
-// An error of half a unit is 2^-21 of a row's reference weight, so that the
+// An error of half a unit is 2^-24 of a row's largest weight, so that the
 // softmax is fp32 throughout in effect, and the sums do not depend on order.
 //
-// One pass: scores are taken relative to a reference, an int32 that starts the
-// products' accumulators at -reference for nothing.  It moves up only when a
-// score exceeds it by more than a factor of 8 (the fixed-point numbers have that
-// room above 1): the sums so far are then folded into fp32 and rescaled, which
-// after a row's first keys hardly ever happens.
+// One pass: scores are taken relative to the largest so far, an int32 that starts
+// the products' accumulators at its negative for nothing.  Where a step brings a
+// larger one, the sums so far are folded into fp32 and rescaled; the other steps
+// (after a row's first keys, most) add integers only.
 #pragma once
 
 #include <climits>
@@ -36,7 +35,7 @@ namespace mnmt {
 constexpr int kAttnKeys = 64;         // keys per step of a wave
 constexpr int kNoReference = -(1 << 22);  // below every score (|s| <= 127^2 128 < 2^21)
 constexpr int kFoldSteps = 1024;      // steps after which the int32 sums are folded: 65536 * 2^14 < 2^31
-constexpr float kLog2One = 19.99f;    // log2 of the fixed-point 1: 8 of it is below 0x7F7F7F, the largest with digits in range
+constexpr float kLog2One = 22.99f;    // log2 of the fixed-point 1, below 0x7F7F7F, the largest number with digits in range
 constexpr float kDigits = 8388608.f + 32896.f;
 constexpr uint32_t kDigitBits = 0x4B008080u;  // its bits: p = 0
 
@@ -121,7 +120,7 @@ struct PagedKeys {
 };
 
 template <int NB, bool PAGED, int WK>
-__global__ __launch_bounds__(256) void k_attn(AttnArgs a) {
+__global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
   constexpr int dh = 16 * NB, KS = (NB + 3) / 4;  // 64-wide slices of the head
   constexpr int kStage = PAGED ? 0 : NB * 1024;   // a wave's values, transposed
   constexpr int kJoin = WK == 1 ? 0 : 16 * (dh + 4) * 4 + 128;
@@ -162,6 +161,7 @@ __global__ __launch_bounds__(256) void k_attn(AttnArgs a) {
         acc[0][b][i] = acc[1][b][i] = acc[2][b][i] = 0;
       }
     int ref = kNoReference, steps = 0;
+    bool folded = false;
     auto fold = [&] {
 #pragma unroll
       for (int b = 0; b < NB; ++b)
@@ -265,16 +265,19 @@ __global__ __launch_bounds__(256) void k_attn(AttnArgs a) {
       }
       top = quad_max(top);
       ++steps;
-      if (__any(top > a.slack) || steps == kFoldSteps) {
-        const int up = top > a.slack ? top : 0;
-        const float scale = __builtin_amdgcn_exp2f(-(float)up * a.c2);
-        fold();
-        steps = 0;
+      if (__any(top > 0) || steps == kFoldSteps) {
+        const int up = max(top, 0);
+        if (steps > 1 || folded) {
+          const float scale = __builtin_amdgcn_exp2f(-(float)up * a.c2);
+          fold();
+          folded = true;
+          steps = 1;
 #pragma unroll
-        for (int b = 0; b < NB; ++b)
+          for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int i = 0; i < 4; ++i) f[b][i] *= scale;
-        sum *= scale;
+            for (int i = 0; i < 4; ++i) f[b][i] *= scale;
+          sum *= scale;
+        }
         ref += up;
 #pragma unroll
         for (int j = 0; j < 4; ++j)

@@ -68,8 +68,6 @@ const char* attn_of(const mnmt_attn_cfg* c, int n_kv_heads, int d_head, AttnArgs
   a->ldo = c->ld_out;
   a->c2 = (float)((double)c->c_qk * 1.44269504088896340736);
   a->c_pv = c->c_pv;
-  // a factor of 8 in score units; scores lie within 2^21 of 0 and the first reference at -2^22
-  a->slack = a->c2 > 0.0f ? (int)std::min(std::floor(3.0 / (double)a->c2), 1e9) : 1000000000;
   return nullptr;
 }
 

@@ -47,7 +47,6 @@ struct AttnArgs {
   const int32_t *start, *len;
   int n, rows, ldq, ldo, group, n_kv_heads, kind, causal;
   float c2, c_pv;  // c_qk log2 e; values' scale
-  int slack;       // score units by which a score may exceed the reference of its row (a factor of 8)
   // the launch: query tiles per row and key head in the grid, key ranges of
   // `chunk` keys per tile, their partial results
   int tiles, splits, chunk;

@@ -8,6 +8,7 @@ library is not built, ``lib()`` raises.
 from __future__ import annotations
 
 import ctypes as C
+import functools
 import os
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -303,25 +304,22 @@ def mnmt_debug_read(x, sink, reps=1, stream=None):
 
 
 # ---- paged cache and attention ---------------------------------------------------------
-def pages_cfg(pool, max_pages: int) -> PagesCfg:
-    """The configuration of a pool int8 [n_layers, n_pages, 2, n_kv_heads, page_size, d_head]: of a page's two halves
-    the first holds the keys in that order, the second the values as [n_kv_heads, page_size / 16, d_head, 16]."""
-    L, n, two, hkv, P, dh = pool.shape
-    _need(two == 2 and pool.dtype == _torch().int8 and pool.is_contiguous(),
+@functools.lru_cache(maxsize=256)
+def _pages(pool_shape, width: int, rows: int):
+    """A pool's configuration (as the C ABI takes it) and the workspace of a fork or compaction of `rows` rows."""
+    _need(len(pool_shape) == 6 and pool_shape[2] == 2,
           "the pool must be a contiguous int8 tensor [n_layers, n_pages, 2, n_kv_heads, page_size, d_head]")
-    return PagesCfg(L, n, P, hkv, dh, max_pages)
+    L, n, _, hkv, P, dh = pool_shape
+    cfg = PagesCfg(L, n, P, hkv, dh, width)
+    return cfg, C.byref(cfg), lib().mnmt_pages_ws_bytes(C.byref(cfg), rows)
 
 
-_torch_module = None
-
-
-def _torch():
-    global _torch_module
-    if _torch_module is None:
-        import torch
-
-        _torch_module = torch
-    return _torch_module
+@functools.lru_cache(maxsize=256)
+def _attn(rows, hkv, dh, d, kind, causal, ld, ldo, most, longest, c_qk, c_pv):
+    """An attention call's configuration and workspace."""
+    _need(dh > 0 and d > 0 and d % dh == 0, "q must have whole heads")
+    a = AttnCfg(d // dh, kind, causal, ld, ldo, most, longest, c_qk, c_pv)
+    return C.byref(a), lib().mnmt_attn_ws_bytes(rows, d // dh, hkv, dh, most, longest)
 
 
 def _need(ok, what):
@@ -329,184 +327,210 @@ def _need(ok, what):
         raise ValueError(what)
 
 
-def _ints(name, t, shape, like):
+def _pool(pool, width, rows):
+    _need(pool.dtype is _int8 and pool.is_contiguous(),
+          "the pool must be a contiguous int8 tensor [n_layers, n_pages, 2, n_kv_heads, page_size, d_head]")
+    return _pages(pool.shape, width, rows)
+
+
+def _ints(name, t, shape, device):
     """Checks an int32 tensor that the kernels read as a dense array."""
-    _need(t.dtype == _torch().int32 and tuple(t.shape) == shape and t.is_contiguous() and t.device == like.device,
-          f"{name} must be a contiguous int32 tensor {list(shape)} on {like.device}")
+    if t.dtype is not _int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != device:
+        raise ValueError(f"{name} must be a contiguous int32 tensor {list(shape)} on device {device}")
 
 
-def _codes(name, t, width, like):
+def _codes(name, t, width, device):
     """Checks int8 rows [n, width] whose columns are adjacent; their stride."""
-    _need(t.dtype == _torch().int8 and t.dim() == 2 and t.shape[1] == width and t.device == like.device
-          and (t.numel() == 0 or t.stride(1) == 1), f"{name} must be int8 [n, {width}] on {like.device}, its columns adjacent")
-    return t.stride(0) if t.shape[0] > 1 else width
+    n, w = t.shape
+    stride, one = t.stride()
+    if t.dtype is not _int8 or w != width or (one != 1 and n and w) or t.get_device() != device:
+        raise ValueError(f"{name} must be int8 [n, {width}] on device {device}, its columns adjacent")
+    return stride if n > 1 else w
 
 
-class _on:
-    """Makes the tensors' device the current one for a call (its stream and its launches belong there)."""
-
-    def __init__(self, t):
-        _need(t.is_cuda, f"the tensors must be on a GPU, not on {t.device}")
-        self.index = t.device.index
-
-    def __enter__(self):
-        cuda = _torch().cuda
-        self.before = cuda.current_device()
-        if self.before != self.index:
-            cuda.set_device(self.index)
-
-    def __exit__(self, *_):
-        if self.before != self.index:
-            _torch().cuda.set_device(self.before)
+def _device(t):
+    """The device of a call; on it the launches and the current stream have to be."""
+    device = t.get_device()
+    _need(device >= 0, f"the tensors must be on a GPU, not on {t.device}")
+    return device
 
 
 def _workspace(nbytes, like, stream):
     """A call's own workspace, so that calls on different streams and captured graphs never share one."""
-    if nbytes == 0:
-        return None
-    t = _torch().empty(nbytes, dtype=_torch().uint8, device=like.device)
+    t = _torch.empty(nbytes, dtype=_torch.uint8, device=like.device)
     if stream is not None:
         t.record_stream(stream)  # (the allocator would give it to the current stream's next call)
     return t
 
 
+def _on_device(f):
+    """Imports torch on the first call, and makes the device of the first tensor the current one for the call."""
+
+    @functools.wraps(f)
+    def call(first, *args, **kw):
+        global _torch, _int8, _int32
+        if _torch is None:
+            import torch
+
+            _int8, _int32, _torch = torch.int8, torch.int32, torch
+        device = first.get_device()
+        if device < 0 or device == _torch.cuda.current_device():
+            return f(first, *args, **kw)
+        with _torch.cuda.device(device):
+            return f(first, *args, **kw)
+
+    return call
+
+
+_torch = _int8 = _int32 = None
+
+
+@_on_device
 def mnmt_pages_fork(pool, table, lens, parent=None, new=None, out=None, stream=None):
     """The next step's tables: row r goes on from row parent[r] (outside the table: empty; None: itself) with room for
     new[r] more tokens.  Returns (table int32 [rows, max_pages], lengths int32 [rows], info int32 [2]: free pages left,
     pages missing); out: these three tensors."""
-    torch = _torch()
     rows_in, width = table.shape
     rows = rows_in if parent is None else parent.shape[0]
-    cfg = pages_cfg(pool, width)
-    _ints("table", table, (rows_in, width), pool)
-    _ints("lens", lens, (rows_in,), pool)
+    _, cfg, nbytes = _pool(pool, width, rows)
+    at = pool.get_device()
+    _ints("table", table, (rows_in, width), at)
+    _ints("lens", lens, (rows_in,), at)
     if parent is not None:
-        _ints("parent", parent, (rows,), pool)
+        _ints("parent", parent, (rows,), at)
     if new is not None:
-        _ints("new", new, (rows,), pool)
-    with _on(pool):
-        if out is None:
-            out = (torch.empty((rows, width), dtype=torch.int32, device=pool.device),
-                   torch.empty(rows, dtype=torch.int32, device=pool.device),
-                   torch.empty(2, dtype=torch.int32, device=pool.device))
-        else:
-            for name, t, shape in zip(("out[0]", "out[1]", "out[2]"), out, ((rows, width), (rows,), (2,))):
-                _ints(name, t, shape, pool)
-        ws = _workspace(lib().mnmt_pages_ws_bytes(C.byref(cfg), rows), pool, stream)
-        rc = lib().mnmt_pages_fork(C.byref(cfg), _ptr(pool), _ptr(table), _ptr(lens), rows_in, _ptr(parent), _ptr(new),
-                                   rows, _ptr(out[0]), _ptr(out[1]), _ptr(out[2]), _ptr(ws),
-                                   0 if ws is None else ws.numel(), _stream(stream))
+        _ints("new", new, (rows,), at)
+    _device(pool)
+    if out is None:
+        # one allocation: the lengths and the counts lie behind the table
+        flat = _torch.empty(rows * (width + 1) + 2, dtype=_int32, device=pool.device)
+        out = (flat[: rows * width].view(rows, width), flat[rows * width: -2], flat[-2:])
+    else:
+        for name, t, shape in zip(("out[0]", "out[1]", "out[2]"), out, ((rows, width), (rows,), (2,))):
+            _ints(name, t, shape, at)
+    ws = _workspace(nbytes, pool, stream)
+    rc = _lib.mnmt_pages_fork(cfg, pool.data_ptr(), table.data_ptr(), lens.data_ptr(), rows_in, _ptr(parent), _ptr(new),
+                              rows, out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), ws.data_ptr(), nbytes,
+                              _stream(stream))
     if rc:
         _check(rc, "mnmt_pages_fork")
     return out
 
 
+@_on_device
 def mnmt_pages_compact(pool, table, lens, out=None, stream=None):
     """Moves the pages in use to the lowest numbers.  Returns (table int32 [rows, max_pages], info int32 [2]: live pages,
     pages moved); out: these two tensors (out[0] may be the table itself)."""
-    torch = _torch()
     rows, width = table.shape
-    cfg = pages_cfg(pool, width)
-    _ints("table", table, (rows, width), pool)
-    _ints("lens", lens, (rows,), pool)
-    with _on(pool):
-        if out is None:
-            out = (torch.empty((rows, width), dtype=torch.int32, device=pool.device),
-                   torch.empty(2, dtype=torch.int32, device=pool.device))
-        else:
-            _ints("out[0]", out[0], (rows, width), pool)
-            _ints("out[1]", out[1], (2,), pool)
-        ws = _workspace(lib().mnmt_pages_ws_bytes(C.byref(cfg), rows), pool, stream)
-        rc = lib().mnmt_pages_compact(C.byref(cfg), _ptr(pool), _ptr(table), _ptr(lens), rows, _ptr(out[0]),
-                                      _ptr(out[1]), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream))
+    _, cfg, nbytes = _pool(pool, width, rows)
+    at = pool.get_device()
+    _ints("table", table, (rows, width), at)
+    _ints("lens", lens, (rows,), at)
+    _device(pool)
+    if out is None:
+        flat = _torch.empty(rows * width + 2, dtype=_int32, device=pool.device)
+        out = (flat[:-2].view(rows, width), flat[-2:])
+    else:
+        _ints("out[0]", out[0], (rows, width), at)
+        _ints("out[1]", out[1], (2,), at)
+    ws = _workspace(nbytes, pool, stream)
+    rc = _lib.mnmt_pages_compact(cfg, pool.data_ptr(), table.data_ptr(), lens.data_ptr(), rows, out[0].data_ptr(),
+                                 out[1].data_ptr(), ws.data_ptr(), nbytes, _stream(stream))
     if rc:
         _check(rc, "mnmt_pages_compact")
     return out
 
 
+@_on_device
 def mnmt_pages_write(pool, layer, table, lens, k, v, start=None, max_q=None, stream=None):
     """Writes the codes k, v int8 [n, n_kv_heads * d_head] of new tokens, the last ones of their rows, into a layer's
     pages; row r has the tokens start[r] .. start[r + 1] - 1 (None: n / rows each), at most max_q as far as known."""
     rows, width = table.shape
-    cfg = pages_cfg(pool, width)
-    _ints("table", table, (rows, width), pool)
-    _ints("lens", lens, (rows,), pool)
-    ld = _codes("k", k, cfg.n_kv_heads * cfg.d_head, pool)
-    n = k.shape[0]
-    _need(_codes("v", v, k.shape[1], pool) == ld and v.shape[0] == n, "k and v must have the same rows and row stride")
+    shape, cfg, _ = _pool(pool, width, rows)
+    at = pool.get_device()
+    _ints("table", table, (rows, width), at)
+    _ints("lens", lens, (rows,), at)
+    d = shape.n_kv_heads * shape.d_head
+    ld, n = _codes("k", k, d, at), k.shape[0]
+    _need(_codes("v", v, d, at) == ld and v.shape[0] == n, "k and v must have the same rows and row stride")
     if start is not None:
-        _ints("start", start, (rows + 1,), pool)
-    with _on(pool):
-        rc = lib().mnmt_pages_write(C.byref(cfg), _ptr(pool), layer, _ptr(table), _ptr(lens), rows, _ptr(k), _ptr(v), ld,
-                                    _ptr(start), n, n if max_q is None else max_q, _stream(stream))
+        _ints("start", start, (rows + 1,), at)
+    _device(pool)
+    rc = _lib.mnmt_pages_write(cfg, pool.data_ptr(), layer, table.data_ptr(), lens.data_ptr(), rows, k.data_ptr(),
+                               v.data_ptr(), ld, _ptr(start), n, n if max_q is None else max_q, _stream(stream))
     if rc:
         _check(rc, "mnmt_pages_write")
 
 
 def _attn_out(q, kind, out):
-    torch = _torch()
-    dt = torch.int8 if kind == ATTN_I8 else torch.float32
+    dt = _int8 if kind == ATTN_I8 else _torch.float32
+    n, d = q.shape
     if out is None:
-        return torch.empty(tuple(q.shape), dtype=dt, device=q.device)
-    _need(out.dtype == dt and out.shape == q.shape and out.device == q.device and (out.numel() == 0 or out.stride(1) == 1),
-          f"out must be {dt} {list(q.shape)} on {q.device}, its columns adjacent")
-    return out
+        return _torch.empty((n, d), dtype=dt, device=q.device), d
+    _need(out.dtype is dt and out.shape == (n, d) and out.device == q.device and (out.numel() == 0 or out.stride(1) == 1),
+          f"out must be {dt} [{n}, {d}] on {q.device}, its columns adjacent")
+    return out, out.stride(0) if n > 1 else d
 
 
+def _most(n, rows, start, max_q):
+    """The most queries of a row, as far as known."""
+    return n // max(rows, 1) if start is None else n if max_q is None or max_q > n else max_q
+
+
+@_on_device
 def mnmt_attn_paged(q, pool, layer, table, lens, c_qk, c_pv, kind=ATTN_F32, start=None, causal=True, max_q=None,
                     max_len=None, out=None, stream=None):
     """Attention of the rows' last tokens, q int8 [n, n_heads * d_head], over a layer's pages: fp32 or (ATTN_I8) int8 of
     q's shape.  Row r has the tokens start[r] .. start[r + 1] - 1 (None: n / rows each); max_q and max_len: the most of
     a row and the longest length, as far as known."""
     rows, width = table.shape
-    cfg = pages_cfg(pool, width)
-    _ints("table", table, (rows, width), pool)
-    _ints("lens", lens, (rows,), pool)
+    shape, cfg, _ = _pool(pool, width, rows)
+    at = pool.get_device()
+    _ints("table", table, (rows, width), at)
+    _ints("lens", lens, (rows,), at)
     n, d = q.shape
-    _need(d > 0 and d % cfg.d_head == 0, "q must have whole heads")
-    ld = _codes("q", q, d, pool)
+    ld = _codes("q", q, d, at)
     if start is not None:
-        _ints("start", start, (rows + 1,), pool)
-    with _on(pool):
-        out = _attn_out(q, kind, out)
-        most = n // max(rows, 1) if start is None else n if max_q is None else min(n, max_q)
-        longest = width * cfg.page_size if max_len is None else min(max_len, width * cfg.page_size)
-        a = AttnCfg(d // cfg.d_head, kind, int(causal), ld, out.stride(0) if n > 1 else d, most,
-                    longest, c_qk, c_pv)
-        ws = _workspace(lib().mnmt_attn_ws_bytes(rows, a.n_heads, cfg.n_kv_heads, cfg.d_head, most, longest), pool, stream)
-        rc = lib().mnmt_attn_paged(C.byref(cfg), C.byref(a), _ptr(pool), layer, _ptr(table), _ptr(lens), rows, _ptr(q),
-                                   _ptr(start), n, _ptr(out), _ptr(ws), 0 if ws is None else ws.numel(), _stream(stream))
+        _ints("start", start, (rows + 1,), at)
+    _device(pool)
+    out, ldo = _attn_out(q, kind, out)
+    longest = width * shape.page_size
+    a, nbytes = _attn(rows, shape.n_kv_heads, shape.d_head, d, kind, 1 if causal else 0, ld, ldo,
+                      _most(n, rows, start, max_q), longest if max_len is None else min(max_len, longest), c_qk, c_pv)
+    ws = _workspace(nbytes, q, stream) if nbytes else None
+    rc = _lib.mnmt_attn_paged(cfg, a, pool.data_ptr(), layer, table.data_ptr(), lens.data_ptr(), rows, q.data_ptr(),
+                              _ptr(start), n, out.data_ptr(), _ptr(ws), nbytes, _stream(stream))
     if rc:
         _check(rc, "mnmt_attn_paged")
     return out
 
 
+@_on_device
 def mnmt_attn_cross(q, k, v, lens, d_head, c_qk, c_pv, kind=ATTN_F32, start=None, max_q=None, out=None, stream=None):
     """Attention of q int8 [n, n_heads * d_head] to the keys and values int8 [rows, S, n_kv_heads * d_head] of each
     query's source sentence, lens[b] of them: fp32 or (ATTN_I8) int8 of q's shape.  Sentence b has the queries
     start[b] .. start[b + 1] - 1 (None: n / rows each), at most max_q as far as known."""
-    torch = _torch()
     rows, S, width = k.shape
     n, d = q.shape
-    _need(d_head > 0 and d % d_head == 0 and width % d_head == 0 and d > 0 and width > 0, "q, k and v must have whole heads")
-    for name, t in (("k", k), ("v", v)):
-        _need(t.dtype == torch.int8 and t.shape == k.shape and t.device == q.device
-              and (t.numel() == 0 or (t.stride() == k.stride() and t.stride(2) == 1)),
-              f"{name} must be int8 [rows, S, n_kv_heads * d_head] on {q.device}, its columns adjacent, k and v strided alike")
-    _ints("lens", lens, (rows,), q)
-    ldq = _codes("q", q, d, q)
+    at = q.get_device()
+    _need(d_head > 0 and width > 0 and width % d_head == 0, "k and v must have whole heads")
+    batch, ld, one = k.stride()
+    if (k.dtype is not _int8 or v.dtype is not _int8 or v.shape != k.shape or k.get_device() != at or v.get_device() != at
+            or (rows and S and (one != 1 or v.stride() != k.stride()))):
+        raise ValueError(f"k and v must be int8 [rows, S, n_kv_heads * d_head] on {q.device}, strided alike, their columns "
+                         "adjacent")
+    _ints("lens", lens, (rows,), at)
+    ldq = _codes("q", q, d, at)
     if start is not None:
-        _ints("start", start, (rows + 1,), q)
+        _ints("start", start, (rows + 1,), at)
+    _device(q)
+    out, ldo = _attn_out(q, kind, out)
     hkv = width // d_head
-    ld = k.stride(1) if S > 1 else width
-    with _on(q):
-        out = _attn_out(q, kind, out)
-        most = n // max(rows, 1) if start is None else n if max_q is None else min(n, max_q)
-        a = AttnCfg(d // d_head, kind, 0, ldq, out.stride(0) if n > 1 else d, most, S, c_qk, c_pv)
-        ws = _workspace(lib().mnmt_attn_ws_bytes(rows, a.n_heads, hkv, d_head, most, S), q, stream)
-        rc = lib().mnmt_attn_cross(C.byref(a), hkv, d_head, _ptr(k), _ptr(v), ld, k.stride(0) if rows > 1 else 0, S,
-                                   _ptr(lens), rows, _ptr(q), _ptr(start), n, _ptr(out), _ptr(ws),
-                                   0 if ws is None else ws.numel(), _stream(stream))
+    a, nbytes = _attn(rows, hkv, d_head, d, kind, 0, ldq, ldo, _most(n, rows, start, max_q), S, c_qk, c_pv)
+    ws = _workspace(nbytes, q, stream) if nbytes else None
+    rc = _lib.mnmt_attn_cross(a, hkv, d_head, k.data_ptr(), v.data_ptr(), ld if S > 1 else width, batch if rows > 1 else 0,
+                              S, lens.data_ptr(), rows, q.data_ptr(), _ptr(start), n, out.data_ptr(), _ptr(ws), nbytes,
+                              _stream(stream))
     if rc:
         _check(rc, "mnmt_attn_cross")
     return out
