@@ -432,8 +432,9 @@ typedef struct {
   float c_qk, c_pv;
 } mnmt_attn_cfg;
 
-/* Workspace of an attention call (0: none is needed).  Host only. */
-size_t mnmt_attn_ws_bytes(int rows, int n_heads, int n_kv_heads, int d_head, int max_q, int max_len);
+/* Workspace of an attention call (0: none is needed), max_len limited to the
+ * table's capacity or S.  Host only. */
+size_t mnmt_attn_ws_bytes(int rows, int n, int n_heads, int n_kv_heads, int d_head, int max_q, int max_len);
 
 /* Attention of a chunk of new tokens of each row over the pages of a layer; a
  * decoding step is a chunk of one token.  d_q int8 [n][ld_q], heads side by

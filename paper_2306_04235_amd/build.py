@@ -22,8 +22,8 @@ COMMON = ["-O3", "-fPIC", "-std=c++17", "-ffp-contract=off", "-Wall", "-Wno-unus
           "-I" + os.path.join(os.path.dirname(HERE), "include")]
 DEVICE = [f"--offload-arch={ARCH}", "-fno-gpu-flush-denormals-to-zero", "-fhip-fp32-correctly-rounded-divide-sqrt",
           "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]
-# per-file device flags: the GEMM keeps its matrix-core accumulators in VGPRs
-EXTRA = {"gemm.hip": ["-mllvm", "-amdgpu-mfma-vgpr-form"]}
+# per-file device flags: matrix-core accumulators in VGPRs
+EXTRA = {f: ["-mllvm", "-amdgpu-mfma-vgpr-form"] for f in ("gemm.hip", "attn_paged.hip", "attn_cross.hip")}
 SOURCES = ["qlinear.hip", "kernels.hip", "decode_fused.hip", "decode_step.hip", "decode_rows.hip", "encode_rows.hip", "encode_small.hip", "gemm.hip", "logits.hip",
            "noalloc.hip", "pages.hip", "attn_paged.hip", "attn_cross.hip", "model.cpp", "session.cpp", "api.cpp", "cache.cpp"]
 

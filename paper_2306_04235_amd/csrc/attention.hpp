@@ -35,7 +35,7 @@ namespace mnmt {
 constexpr int kAttnKeys = 64;         // keys per step of a wave
 constexpr int kNoReference = -(1 << 22);  // below every score (|s| <= 127^2 128 < 2^21)
 constexpr int kFoldSteps = 1024;      // steps after which the int32 sums are folded: 65536 * 2^14 < 2^31
-constexpr float kLog2One = 22.99f;    // log2 of the fixed-point 1, below 0x7F7F7F, the largest number with digits in range
+constexpr float kOne = 8355711.f;     // the fixed-point 1: 0x7F7F7F, the largest number with digits in range
 constexpr float kDigits = 8388608.f + 32896.f;
 constexpr uint32_t kDigitBits = 0x4B008080u;  // its bits: p = 0
 
@@ -82,8 +82,14 @@ __device__ __forceinline__ AttnRow attn_row(const AttnArgs& a, int r) {
 __device__ __forceinline__ int tile_keys(const AttnArgs& a, const AttnRow& w, int tile) {
   return w.seen(a, min(w.n - 1, (16 * tile + 15) / a.group));
 }
-__device__ __forceinline__ int live_splits(const AttnArgs& a, int tile, int keys) {
-  return tile < a.tiles ? min(a.splits, max(1, (keys + a.chunk - 1) / a.chunk)) : 1;
+__device__ __forceinline__ int live_splits(const AttnArgs& a, int keys) {
+  return min(a.splits, max(1, (keys + a.chunk - 1) / a.chunk));
+}
+// Place of a tile's key range in the workspace: rows' tiles one after the other,
+// whatever the rows' sizes are (row r begins at a token's tile or behind it).
+__device__ __forceinline__ size_t tile_slot(const AttnArgs& a, const AttnRow& w, int row, int head, int tile, int split) {
+  const size_t slot = (size_t)w.first * a.group / 16 + row + tile;
+  return (slot * a.n_kv_heads + head) * a.splits + split;
 }
 
 // Where a lane finds its keys and values: pages, values [token / 16][dh][16].
@@ -119,6 +125,195 @@ struct PagedKeys {
   }
 };
 
+// Four columns of query m of a row and key head, from joined sums.
+__device__ __forceinline__ void store_joined(const AttnArgs& a, const AttnRow& w, int kv_head, int m, int c, int dh,
+                                             float4 y, float sum) {
+  const int token = m / a.group;
+  if (token >= w.n) return;
+  const float inv = sum > 0.f ? a.c_pv / sum : 0.f;
+  const size_t o = ((size_t)w.first + token) * a.ldo + (size_t)(kv_head * a.group + m - token * a.group) * dh + c;
+  if (a.kind == MNMT_ATTN_F32)
+    *(float4*)((float*)a.out + o) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
+  else
+    *(char4*)((int8_t*)a.out + o) =
+        make_char4(code_of(y.x * inv), code_of(y.y * inv), code_of(y.z * inv), code_of(y.w * inv));
+}
+
+// The lane's query of a tile.
+template <int NB>
+struct TileQuery {
+  bool real;
+  int mine;      // keys it sees
+  size_t out;    // its row of q and of out
+  int head;
+  v4i q[(NB + 3) / 4];
+  __device__ __forceinline__ void load(const AttnArgs& a, const AttnRow& w, int kv_head, int tile, int lane) {
+    constexpr int dh = 16 * NB;
+    const int m = 16 * tile + (lane & 15), token = m / a.group;
+    real = token < w.n;
+    mine = real ? w.seen(a, token) : INT_MAX;
+    out = (size_t)w.first + (real ? token : 0);
+    head = kv_head * a.group + (real ? m - token * a.group : 0);
+#pragma unroll
+    for (int s = 0; s < (NB + 3) / 4; ++s) {
+      const int c = 64 * s + 16 * (lane >> 4);
+      q[s] = c < dh && real ? *(const v4i*)(a.q + out * a.ldq + (size_t)head * dh + c) : v4i{0, 0, 0, 0};
+    }
+  }
+};
+
+// The sums of a query tile: columns 16 b + 4 (lane / 16) + i of query lane % 16.
+template <int NB>
+struct TileSums {
+  v4i acc[3][NB];  // digits' products since the last fold
+  float f[NB][4], sum;
+  int ref, steps;
+  bool folded;
+
+  __device__ __forceinline__ TileSums() : sum(0.f), ref(kNoReference), steps(0), folded(false) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[b][i] = 0.f;
+        acc[0][b][i] = acc[1][b][i] = acc[2][b][i] = 0;
+      }
+  }
+  __device__ __forceinline__ void fold() {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        f[b][i] = fmaf(65536.f, (float)acc[0][b][i], f[b][i]);
+        f[b][i] = fmaf(256.f, (float)acc[1][b][i], f[b][i]);
+        f[b][i] += (float)acc[2][b][i];
+        acc[0][b][i] = acc[1][b][i] = acc[2][b][i] = 0;
+      }
+  }
+  // The lane's largest; what is masked becomes INT_MIN / 2.
+  static __device__ __forceinline__ int largest(v4i (&d)[4], bool masked, int count) {
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          int v = 4 * j + i >= count ? INT_MIN / 2 : d[j][i];
+          asm volatile("" : "+v"(v));  // (stays in this branch: as a select it would cost every step)
+          d[j][i] = v;
+        }
+    }
+    int top = max(max(d[0][0], d[0][1]), d[0][2]);
+    top = max(top, d[0][3]);
+#pragma unroll
+    for (int j = 1; j < 4; ++j) {
+      top = max(max(top, d[j][0]), d[j][1]);
+      top = max(max(top, d[j][2]), d[j][3]);
+    }
+    return top;
+  }
+  // Weights of a step: d[j][i] = score less ref of the lane's query and key 4 j + i
+  // of its 16, of which the first `count` are seen (all where not masked); p: the
+  // weights' digits.
+  __device__ __forceinline__ void weigh(v4i (&d)[4], bool masked, int count, float c2, v4i (&p)[3]) {
+    int top = quad_max(largest(d, masked, count));
+    ++steps;
+    if (__any(top > 0) || steps == kFoldSteps) {
+      const int up = max(top, 0);
+      if (steps > 1 || folded) {
+        const float scale = __builtin_amdgcn_exp2f(-(float)up * c2);
+        fold();
+        folded = true;
+        steps = 1;
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f[b][i] *= scale;
+        sum *= scale;
+      }
+      ref += up;
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[j][i] -= up;  // (masked places stay far below)
+    }
+    float x[4][4];
+    exponents(d, masked, count, c2, x);
+    digits(x, p);
+  }
+  // Exponents c2 d; -inf where masked.
+  static __device__ __forceinline__ void exponents(const v4i (&d)[4], bool masked, int count, float c2,
+                                                   float (&x)[4][4]) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) x[j][i] = (float)d[j][i] * c2;
+    if (masked) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          x[j][i] = 4 * j + i >= count ? -__builtin_inff() : x[j][i];
+          asm volatile("" : "+v"(x[j][i]));
+        }
+    }
+  }
+  // Digits of the weights 2^x.
+  __device__ __forceinline__ void digits(const float (&x)[4][4], v4i (&p)[3]) {
+    uint32_t total = 0;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      uint32_t u[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        u[i] = __float_as_uint(fmaf(__builtin_amdgcn_exp2f(x[j][i]), kOne, kDigits));
+        total += u[i];
+      }
+      const uint32_t lo0 = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
+      const uint32_t hi0 = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0602u), hi1 = __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0602u);
+      p[0][j] = (int)__builtin_amdgcn_perm(hi1, hi0, 0x05040100u);
+      p[1][j] = (int)(__builtin_amdgcn_perm(lo1, lo0, 0x07060302u) ^ 0x80808080u);
+      p[2][j] = (int)(__builtin_amdgcn_perm(lo1, lo0, 0x05040100u) ^ 0x80808080u);
+    }
+    sum += (float)(total - 16u * kDigitBits);
+  }
+  __device__ __forceinline__ void add(int b, v4i values, const v4i (&p)[3]) {
+#pragma unroll
+    for (int x = 0; x < 3; ++x) acc[x][b] = mfma16(values, p[x], acc[x][b]);
+  }
+  // After the last step: the query's outputs, or its partial result [16][dh], sums [16], references [16].
+  __device__ __forceinline__ void close() {
+    fold();
+    sum = quad_sum(sum);
+  }
+  __device__ __forceinline__ void store(const AttnArgs& a, const TileQuery<NB>& t, int lane) const {
+    if (!t.real) return;
+    const float inv = sum > 0.f ? a.c_pv / sum : 0.f;
+    const size_t o = t.out * a.ldo + (size_t)t.head * (16 * NB) + 4 * (lane >> 4);
+#pragma unroll
+    for (int b = 0; b < NB; ++b) {
+      const float x0 = f[b][0] * inv, x1 = f[b][1] * inv, x2 = f[b][2] * inv, x3 = f[b][3] * inv;
+      if (a.kind == MNMT_ATTN_F32)
+        *(float4*)((float*)a.out + o + 16 * b) = make_float4(x0, x1, x2, x3);
+      else
+        *(char4*)((int8_t*)a.out + o + 16 * b) = make_char4(code_of(x0), code_of(x1), code_of(x2), code_of(x3));
+    }
+  }
+  __device__ __forceinline__ void store_part(float* part, int lane) const {
+    constexpr int dh = 16 * NB;
+    const int col = lane & 15, g = lane >> 4;
+    if (g == 0) {
+      part[16 * dh + col] = sum;
+      part[16 * dh + 16 + col] = (float)ref;
+    }
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+      *(float4*)(part + col * dh + 16 * b + 4 * g) = make_float4(f[b][0], f[b][1], f[b][2], f[b][3]);
+  }
+};
+
+// One query tile per wave (WK 1) or per block, whose four waves take turns at
+// the keys (WK 4).  For few queries per row: every wave loads its keys and
+// values straight into the matrix operands.
 template <int NB, bool PAGED, int WK>
 __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
   constexpr int dh = 16 * NB, KS = (NB + 3) / 4;  // 64-wide slices of the head
@@ -135,44 +330,13 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
   const int split = unit % per_head / a.tiles, tile0 = a.tiles - 1 - unit % a.tiles;
   const AttnRow w = attn_row(a, row);
   for (int tile = tile0; 16 * tile < w.n * a.group; tile += a.tiles) {
-    const int keys = tile_keys(a, w, tile), live = live_splits(a, tile, keys);
+    const int keys = tile_keys(a, w, tile), live = live_splits(a, keys);
     if (split >= live) continue;
     const int kbegin = split * a.chunk, kend = split == live - 1 ? keys : kbegin + a.chunk;
-    const int all_see = w.seen(a, 16 * tile / a.group);  // keys that every query of the tile sees
-    // the lane's query
-    const int m = 16 * tile + col, token = m / a.group;
-    const bool real = token < w.n;
-    const int mine = real ? w.seen(a, token) : INT_MAX;
-    const size_t qrow = (size_t)w.first + (real ? token : 0);
-    const int qhead = head * a.group + (real ? m - token * a.group : 0);
-    v4i qf[KS];
-#pragma unroll
-    for (int s = 0; s < KS; ++s) {
-      const int c = 64 * s + 16 * g;
-      qf[s] = c < dh && real ? *(const v4i*)(a.q + qrow * a.ldq + (size_t)qhead * dh + c) : v4i{0, 0, 0, 0};
-    }
-    v4i acc[3][NB];
-    float f[NB][4], sum = 0.f;
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f[b][i] = 0.f;
-        acc[0][b][i] = acc[1][b][i] = acc[2][b][i] = 0;
-      }
-    int ref = kNoReference, steps = 0;
-    bool folded = false;
-    auto fold = [&] {
-#pragma unroll
-      for (int b = 0; b < NB; ++b)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          f[b][i] = fmaf(65536.f, (float)acc[0][b][i], f[b][i]);
-          f[b][i] = fmaf(256.f, (float)acc[1][b][i], f[b][i]);
-          f[b][i] += (float)acc[2][b][i];
-          acc[0][b][i] = acc[1][b][i] = acc[2][b][i] = 0;
-        }
-    };
+    const int all_see = min(w.seen(a, 16 * tile / a.group), kend);  // keys that every query of the tile sees
+    TileQuery<NB> t;
+    t.load(a, w, head, tile, lane);
+    TileSums<NB> y;
     // key rows of the lane in a step: 16 (l / 4 mod 4) + 4 j + l mod 4; slices past the head read its first bytes (their queries are 0)
     int slice[KS];
 #pragma unroll
@@ -221,12 +385,12 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
             for (int c = 0; c < 4; ++c) {
               const uint32_t x[4] = {(uint32_t)vr[0][s][c], (uint32_t)vr[1][s][c], (uint32_t)vr[2][s][c],
                                      (uint32_t)vr[3][s][c]};
-              uint32_t y[4];
-              transpose4(x, y[0], y[1], y[2], y[3]);
+              uint32_t z[4];
+              transpose4(x, z[0], z[1], z[2], z[3]);
               // column 64 s + 16 g + 4 c + b: chunk (col / 4) ^ c ^ g
 #pragma unroll
               for (int b = 0; b < 4; ++b)
-                *(uint32_t*)(stage + (64 * s + 16 * g + 4 * c + b) * 64 + 16 * ((col >> 2) ^ c ^ g) + 4 * (col & 3)) = y[b];
+                *(uint32_t*)(stage + (64 * s + 16 * g + 4 * c + b) * 64 + 16 * ((col >> 2) ^ c ^ g) + 4 * (col & 3)) = z[b];
             }
           }
         }
@@ -240,121 +404,39 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
         __builtin_amdgcn_wave_barrier();
       }
       // scores less the reference: the lane's query, keys key + 16 g + 4 j + i
-      v4i d[4];
+      v4i d[4], p[3];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        d[j] = mfma16(kf[j][0], qf[0], v4i{-ref, -ref, -ref, -ref});
+        d[j] = mfma16(kf[j][0], t.q[0], v4i{-y.ref, -y.ref, -y.ref, -y.ref});
 #pragma unroll
-        for (int s = 1; s < KS; ++s) d[j] = mfma16(kf[j][s], qf[s], d[j]);
+        for (int s = 1; s < KS; ++s) d[j] = mfma16(kf[j][s], t.q[s], d[j]);
       }
-      const int k0 = key + 16 * g, last = min(mine, kend);
-      const bool masked = key + kAttnKeys > min(all_see, kend) || __any(!there);
-      if (masked) {
+      y.weigh(d, key + kAttnKeys > all_see || __any(!there), there ? min(t.mine, kend) - key - 16 * g : 0, a.c2, p);
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (!there || k0 + 4 * j + i >= last) d[j][i] = INT_MIN / 2;
-      }
-      int top = max(max(d[0][0], d[0][1]), d[0][2]);
-      top = max(top, d[0][3]);
-#pragma unroll
-      for (int j = 1; j < 4; ++j) {
-        top = max(max(top, d[j][0]), d[j][1]);
-        top = max(max(top, d[j][2]), d[j][3]);
-      }
-      top = quad_max(top);
-      ++steps;
-      if (__any(top > 0) || steps == kFoldSteps) {
-        const int up = max(top, 0);
-        if (steps > 1 || folded) {
-          const float scale = __builtin_amdgcn_exp2f(-(float)up * a.c2);
-          fold();
-          folded = true;
-          steps = 1;
-#pragma unroll
-          for (int b = 0; b < NB; ++b)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) f[b][i] *= scale;
-          sum *= scale;
-        }
-        ref += up;
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) d[j][i] -= up;  // (masked places stay far below)
-      }
-      uint32_t total = 0;
-      v4i pa, pb, pc;
-#pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        uint32_t x[4];
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[i] = __float_as_uint(__builtin_amdgcn_exp2f(fmaf((float)d[j][i], a.c2, kLog2One)) + kDigits);
-          if (masked && (!there || k0 + 4 * j + i >= last)) x[i] = kDigitBits;
-          total += x[i];
-        }
-        const uint32_t lo0 = __builtin_amdgcn_perm(x[1], x[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(x[3], x[2], 0x05010400u);
-        const uint32_t hi0 = __builtin_amdgcn_perm(x[1], x[0], 0x0c0c0602u), hi1 = __builtin_amdgcn_perm(x[3], x[2], 0x0c0c0602u);
-        pc[j] = (int)(__builtin_amdgcn_perm(lo1, lo0, 0x05040100u) ^ 0x80808080u);
-        pb[j] = (int)(__builtin_amdgcn_perm(lo1, lo0, 0x07060302u) ^ 0x80808080u);
-        pa[j] = (int)__builtin_amdgcn_perm(hi1, hi0, 0x05040100u);
-      }
-      sum += (float)(total - 16u * kDigitBits);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) {
-        acc[0][b] = mfma16(vf[b], pa, acc[0][b]);
-        acc[1][b] = mfma16(vf[b], pb, acc[1][b]);
-        acc[2][b] = mfma16(vf[b], pc, acc[2][b]);
-      }
+      for (int b = 0; b < NB; ++b) y.add(b, vf[b], p);
     }
-    fold();
-    sum = quad_sum(sum);
-    // f: columns 16 b + 4 g + i of the lane's query
-    float* part = a.part + ((size_t)(row * a.n_kv_heads + head) * a.tiles + tile) * a.splits * (16 * (dh + 2)) +
-                  (size_t)split * (16 * (dh + 2));
+    y.close();
     if constexpr (WK == 1) {
-      if (live == 1) {
-        if (real) {
-          const float inv = sum > 0.f ? a.c_pv / sum : 0.f;
-          const size_t o = qrow * a.ldo + (size_t)qhead * dh + 4 * g;
-#pragma unroll
-          for (int b = 0; b < NB; ++b) {
-            if (a.kind == MNMT_ATTN_F32) {
-              *(float4*)((float*)a.out + o + 16 * b) =
-                  make_float4(f[b][0] * inv, f[b][1] * inv, f[b][2] * inv, f[b][3] * inv);
-            } else {
-              char4 c = make_char4(code_of(f[b][0] * inv), code_of(f[b][1] * inv), code_of(f[b][2] * inv),
-                                   code_of(f[b][3] * inv));
-              *(char4*)((int8_t*)a.out + o + 16 * b) = c;
-            }
-          }
-        }
-      } else {
-        if (g == 0) {
-          part[16 * dh + col] = sum;
-          part[16 * dh + 16 + col] = (float)ref;
-        }
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-          *(float4*)(part + col * dh + 16 * b + 4 * g) = make_float4(f[b][0], f[b][1], f[b][2], f[b][3]);
-      }
+      if (live == 1)
+        y.store(a, t, lane);
+      else
+        y.store_part(a.part + tile_slot(a, w, row, head, tile, split) * (16 * (dh + 2)), lane);
     } else {
       // join the four waves' sums, each relative to its own reference
       float* mine_f = (float*)(lds + wave * kWave);
       if (g == 0) {
-        mine_f[col] = sum;
-        mine_f[16 + col] = (float)ref;
+        mine_f[col] = y.sum;
+        mine_f[16 + col] = (float)y.ref;
       }
 #pragma unroll
       for (int b = 0; b < NB; ++b)
-        *(float4*)(mine_f + 32 + col * (dh + 4) + 16 * b + 4 * g) = make_float4(f[b][0], f[b][1], f[b][2], f[b][3]);
+        *(float4*)(mine_f + 32 + col * (dh + 4) + 16 * b + 4 * g) = make_float4(y.f[b][0], y.f[b][1], y.f[b][2], y.f[b][3]);
       __syncthreads();
+      float* part = a.part + tile_slot(a, w, row, head, tile, split) * (16 * (dh + 2));
       for (int i = threadIdx.x; i < 16 * dh / 4; i += 256) {
         const int q = i / (dh / 4), c = 4 * (i % (dh / 4));
         float top = (float)kNoReference, wsum = 0.f;
-        float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+        float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
         for (int v = 0; v < 4; ++v) top = fmaxf(top, ((const float*)(lds + v * kWave))[16 + q]);
 #pragma unroll
@@ -363,31 +445,335 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
           const float scale = __builtin_amdgcn_exp2f((src[16 + q] - top) * a.c2);
           const float4 x = *(const float4*)(src + 32 + q * (dh + 4) + c);
           wsum = fmaf(scale, src[q], wsum);
-          y.x = fmaf(scale, x.x, y.x);
-          y.y = fmaf(scale, x.y, y.y);
-          y.z = fmaf(scale, x.z, y.z);
-          y.w = fmaf(scale, x.w, y.w);
+          o.x = fmaf(scale, x.x, o.x);
+          o.y = fmaf(scale, x.y, o.y);
+          o.z = fmaf(scale, x.z, o.z);
+          o.w = fmaf(scale, x.w, o.w);
         }
         if (live == 1) {
-          const int mq = 16 * tile + q, tq = mq / a.group;
-          if (tq < w.n) {
-            const float inv = wsum > 0.f ? a.c_pv / wsum : 0.f;
-            const size_t o = ((size_t)w.first + tq) * a.ldo + (size_t)(head * a.group + mq - tq * a.group) * dh + c;
-            if (a.kind == MNMT_ATTN_F32)
-              *(float4*)((float*)a.out + o) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
-            else
-              *(char4*)((int8_t*)a.out + o) =
-                  make_char4(code_of(y.x * inv), code_of(y.y * inv), code_of(y.z * inv), code_of(y.w * inv));
-          }
+          store_joined(a, w, head, 16 * tile + q, c, dh, o, wsum);
         } else {
           if (c == 0) {
             part[16 * dh + q] = wsum;
             part[16 * dh + 16 + q] = top;
           }
-          *(float4*)(part + q * dh + c) = y;
+          *(float4*)(part + q * dh + c) = o;
         }
       }
       __syncthreads();
+    }
+  }
+}
+
+// The largest score of each query of a few tiles over a range of keys: the waves
+// take turns at the keys, straight from memory, one step ahead in registers, each
+// step against all of the block's queries.
+constexpr int top_tiles(int nb) { return nb <= 4 ? 8 : 4; }  // (their queries stay in registers)
+
+template <int NB, bool PAGED>
+__global__ __launch_bounds__(256, 2) void k_attn_top(AttnArgs a) {
+  constexpr int dh = 16 * NB, KS = (NB + 3) / 4, kStride = 4 * kAttnKeys, kTopTiles = top_tiles(NB);
+  __shared__ int tops[4 * kTopTiles * 16];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
+  const int groups = a.tiles / kTopTiles, per_head = groups * a.splits, per_row = per_head * a.n_kv_heads;
+  const int row = blockIdx.x / per_row, head = blockIdx.x % per_row / per_head;
+  const int split = blockIdx.x % per_head / groups, group0 = groups - 1 - blockIdx.x % groups;
+  const AttnRow w = attn_row(a, row);
+  const int tiles = (w.n * a.group + 15) / 16;
+  int slice[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) slice[s] = 64 * s + 16 * g < dh ? 64 * s + 16 * g : 0;
+  for (int group = group0; kTopTiles * group < tiles; group += groups) {
+    const int tile = kTopTiles * group;
+    // (the chunk kernel's ranges: by its blocks' last tiles, which see no more than this block's)
+    const int keys = tile_keys(a, w, min(tile + kTopTiles, tiles) - 1), live = live_splits(a, keys);
+    if (split >= live) continue;
+    const int kbegin = split * a.chunk, kend = split == live - 1 ? keys : kbegin + a.chunk;
+    const int all_see = min(w.seen(a, 16 * tile / a.group), kend);
+    v4i q[kTopTiles][KS];
+    int seen[kTopTiles], top[kTopTiles];
+#pragma unroll
+    for (int x = 0; x < kTopTiles; ++x) {
+      TileQuery<NB> t;
+      t.load(a, w, head, min(tile + x, tiles), lane);
+#pragma unroll
+      for (int s = 0; s < KS; ++s) q[x][s] = t.q[s];
+      seen[x] = min(t.mine, kend);
+      top[x] = kNoReference;
+    }
+    PagedKeys<NB> at(a, PAGED ? row : 0, head, lane, kend);
+    const int8_t* kbase = PAGED ? nullptr : a.k + (size_t)row * a.batch + (size_t)head * dh;
+    v4i k[4][KS];
+    bool there = true;
+    auto look = [&](int key) {
+      if constexpr (PAGED) at.look(min(key, kend - 1));
+    };
+    auto load = [&](int key) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int8_t* kp;
+        if constexpr (PAGED)
+          kp = at.keys_of(key) + 4 * j * dh;
+        else
+          kp = kbase + (size_t)min(key + 16 * ((lane >> 2) & 3) + 4 * j + (lane & 3), kend - 1) * a.ld;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) k[j][s] = *(const v4i*)(kp + slice[s]);
+      }
+      if constexpr (PAGED) there = at.there();
+    };
+    int key = kbegin + kAttnKeys * wave;
+    if (key < kend) {
+      look(key);
+      load(key);
+      look(key + kStride);
+    }
+    while (key < kend) {
+      v4i kc[4][KS];
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kc[j][s] = k[j][s];
+      const bool here = there, masked = key + kAttnKeys > all_see || __any(!here);
+      const int now = key;
+      key += kStride;
+      if (key < kend) {
+        load(key);
+        look(key + kStride);
+      }
+#pragma unroll
+      for (int x = 0; x < kTopTiles; ++x) {
+        v4i d[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          d[j] = mfma16(kc[j][0], q[x][0], v4i{0, 0, 0, 0});
+#pragma unroll
+          for (int s = 1; s < KS; ++s) d[j] = mfma16(kc[j][s], q[x][s], d[j]);
+        }
+        top[x] = max(top[x], TileSums<NB>::largest(d, masked, here ? seen[x] - now - 16 * g : 0));
+      }
+    }
+#pragma unroll
+    for (int x = 0; x < kTopTiles; ++x) {
+      const int m = quad_max(top[x]);
+      if (g == 0) tops[(wave * kTopTiles + x) * 16 + lane] = m;
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < kTopTiles * 16; i += 256) {
+      int m = tops[i];
+#pragma unroll
+      for (int v = 1; v < 4; ++v) m = max(m, tops[v * kTopTiles * 16 + i]);
+      if (tile + i / 16 < tiles) a.tops[tile_slot(a, w, row, head, tile + i / 16, split) * 16 + i % 16] = m;
+    }
+    __syncthreads();
+  }
+}
+
+// The query tiles of four waves, over the same keys: 64 of them at a time pass
+// through LDS, in the order of the matrix operands (a kilobyte per operand, lane
+// by lane), so that a block reads them once.  A wave has two tiles where its
+// registers hold their sums at two waves per SIMD (heads of up to 64), and reads
+// each operand for both.  Keys, and the values of pages, come in by loads
+// straight to LDS, one step ahead; an encoder's values are transposed on the way,
+// each wave those of its 16 keys.
+//
+// The references are the scores' maxima, from k_attn_top: they never move, so that
+// the sums are integers throughout and no step branches.
+constexpr int chunk_tiles(int nb) { return nb <= 4 ? 2 : 1; }  // of a wave
+constexpr int kValueGap = 16;  // between values' operands: the transposing stores meet no bank conflicts
+
+__device__ __forceinline__ void load_to_lds(const int8_t* from, int8_t* to) {  // 16 bytes per lane, to + 16 lane
+  __builtin_amdgcn_global_load_lds((const __attribute__((address_space(1))) void*)from,
+                                   (__attribute__((address_space(3))) void*)to, 16, 0, 0);
+}
+
+// Waits for the wave's loads to LDS, then for the block's other waves.
+__device__ __forceinline__ void landed() {
+  asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+  __syncthreads();
+}
+
+// LONG: ranges may hold more keys than the int32 sums (kFoldSteps); without it no
+// register holds sums in fp32 meanwhile.
+template <int NB, bool PAGED, bool LONG>
+__global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
+  constexpr int dh = 16 * NB, KS = (NB + 3) / 4, QT = chunk_tiles(NB), kTiles = 4 * QT;
+  constexpr int kKeyBytes = 4 * KS * 1024, kValueBytes = NB * (1024 + kValueGap);
+  __shared__ __attribute__((aligned(16))) int8_t kbuf[2 * kKeyBytes], vbuf[3 * kValueBytes];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int g = lane >> 4;
+  // blocks of one row and head side by side, so that the L2s hold what they read,
+  // the last tiles first (in a causal chunk they see most)
+  const int groups = a.tiles / kTiles, per_head = groups * a.splits, per_row = per_head * a.n_kv_heads;
+  const int row = blockIdx.x / per_row, head = blockIdx.x % per_row / per_head;
+  const int split = blockIdx.x % per_head / groups, group0 = groups - 1 - blockIdx.x % groups;
+  const AttnRow w = attn_row(a, row);
+  const int tiles = (w.n * a.group + 15) / 16;
+  int slice[KS];
+#pragma unroll
+  for (int s = 0; s < KS; ++s) slice[s] = 64 * s + 16 * g < dh ? 64 * s + 16 * g : 0;
+  for (int group = group0; kTiles * group < tiles; group += groups) {
+    // ranges of keys by the block's last tile; a tile that sees fewer keys has nothing in the last ones
+    const int tile = kTiles * group + QT * wave;
+    const int block_keys = tile_keys(a, w, min(kTiles * (group + 1), tiles) - 1);
+    const int live = live_splits(a, block_keys);
+    if (split >= live) continue;
+    const int kbegin = split * a.chunk, kend = split == live - 1 ? block_keys : kbegin + a.chunk;
+    // the keys that every query of the wave's tiles sees
+    const int all_see = tile < tiles ? min(w.seen(a, 16 * tile / a.group), kend) : 0;
+    TileQuery<NB> t[QT];
+#pragma unroll
+    for (int x = 0; x < QT; ++x) t[x].load(a, w, head, min(tile + x, tiles), lane);
+    TileSums<NB> y[QT];
+    PagedKeys<NB> at(a, PAGED ? row : 0, head, lane, kend);
+    const int8_t* kbase = PAGED ? nullptr : a.k + (size_t)row * a.batch + (size_t)head * dh;
+    const int8_t* vbase = PAGED ? nullptr : a.v + (size_t)row * a.batch + (size_t)head * dh;
+    const int dc = lane >> 2, kg = lane & 3;  // transposing: 16 columns, 4 keys of the wave's 16
+    v4i vr[4];
+    bool there = true, next_there = true;
+    auto fetch_keys = [&](int key, int8_t* buf) {  // operand (j, s) of keys 16 (l / 4 mod 4) + 4 j + l mod 4
+      const int8_t* kp;
+      if constexpr (PAGED) {
+        kp = at.keys_of(key) + 4 * wave * dh;
+        next_there = at.there();
+      } else {
+        kp = kbase + (size_t)min(key + 16 * ((lane >> 2) & 3) + 4 * wave + (lane & 3), kend - 1) * a.ld;
+      }
+#pragma unroll
+      for (int s = 0; s < KS; ++s) load_to_lds(kp + slice[s], buf + (wave * KS + s) * 1024);
+    };
+    auto fetch_values = [&](int key, int8_t* buf) {
+      if constexpr (PAGED) {
+        const int8_t* vp = at.values_of(key);
+#pragma unroll
+        for (int b = 0; b < NB; b += 4)
+          if (b + wave < NB) load_to_lds(vp + 256 * (b + wave), buf + (b + wave) * (1024 + kValueGap));
+      } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          if (dc < NB) vr[i] = *(const v4i*)(vbase + (size_t)min(key + 16 * wave + 4 * kg + i, kend - 1) * a.ld + 16 * dc);
+      }
+    };
+    auto transpose = [&](int8_t* buf) {  // the values that fetch_values left in registers
+      if constexpr (!PAGED) {
+        if (dc < NB) {
+          uint32_t* to = (uint32_t*)(buf + dc * (1024 + kValueGap) + 256 * wave) + kg;
+#pragma unroll
+          for (int c = 0; c < 4; ++c) {
+            const uint32_t x[4] = {(uint32_t)vr[0][c], (uint32_t)vr[1][c], (uint32_t)vr[2][c], (uint32_t)vr[3][c]};
+            uint32_t z[4];
+            transpose4(x, z[0], z[1], z[2], z[3]);
+#pragma unroll
+            for (int b = 0; b < 4; ++b) to[4 * (4 * c + b)] = z[b];
+          }
+        }
+      }
+    };
+    auto look = [&](int key) {
+      if constexpr (PAGED) at.look(min(key, kend - 1));
+    };
+    auto scores = [&](const int8_t* buf, v4i (&d)[QT][4], const int (&ref)[QT]) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        v4i k[KS];
+#pragma unroll
+        for (int s = 0; s < KS; ++s) k[s] = *(const v4i*)(buf + (j * KS + s) * 1024 + 16 * lane);
+#pragma unroll
+        for (int x = 0; x < QT; ++x) {
+          d[x][j] = mfma16(k[0], t[x].q[0], v4i{-ref[x], -ref[x], -ref[x], -ref[x]});
+#pragma unroll
+          for (int s = 1; s < KS; ++s) d[x][j] = mfma16(k[s], t[x].q[s], d[x][j]);
+        }
+      }
+    };
+    __syncthreads();  // (the last group's reads of LDS are over)
+    if (kbegin < kend) {
+      int ref[QT], cur = 0;
+#pragma unroll
+      for (int x = 0; x < QT; ++x)
+        ref[x] = y[x].ref =
+            tile + x < tiles ? a.tops[tile_slot(a, w, row, head, tile + x, split) * 16 + (lane & 15)] : kNoReference;
+      // the weights of a step, and the products of the step before, which need
+      // nothing of it: the matrix and the vector unit work side by side
+      look(kbegin);
+      fetch_keys(kbegin, kbuf);
+      fetch_values(kbegin, vbuf);
+      look(kbegin + kAttnKeys);
+      transpose(vbuf);
+      v4i p[QT][3];
+      int8_t *v_prev = vbuf + 2 * kValueBytes, *v_cur = vbuf, *v_next = vbuf + kValueBytes;
+      auto values = [&](v4i (&v)[NB]) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b) v[b] = *(const v4i*)(v_prev + b * (1024 + kValueGap) + 16 * lane);
+      };
+      auto products = [&](const v4i (&v)[NB]) {
+#pragma unroll
+        for (int b = 0; b < NB; ++b)
+#pragma unroll
+          for (int x = 0; x < QT; ++x) y[x].add(b, v[b], p[x]);
+      };
+      int key = kbegin;
+      do {
+        const int pend = LONG ? min(kend - key, kAttnKeys * kFoldSteps) + key : kend;
+#pragma unroll
+        for (int x = 0; x < QT; ++x)
+#pragma unroll
+          for (int i = 0; i < 3; ++i) p[x][i] = v4i{0, 0, 0, 0};
+        for (; key < pend; key += kAttnKeys, cur ^= 1) {
+          there = next_there;
+          landed();
+          const bool more = key + kAttnKeys < kend;
+          v4i d[QT][4], v[NB];
+          float x[QT][4][4];
+          scores(kbuf + cur * kKeyBytes, d, ref);
+          values(v);
+          // nothing is read from LDS between here and the next step: a read would
+          // wait for these loads
+          if (more) {
+            fetch_keys(key + kAttnKeys, kbuf + (cur ^ 1) * kKeyBytes);
+            fetch_values(key + kAttnKeys, v_next);
+            look(key + 2 * kAttnKeys);
+          }
+          const bool masked = key + kAttnKeys > all_see || __any(!there);
+#pragma unroll
+          for (int i = 0; i < QT; ++i)
+            TileSums<NB>::exponents(d[i], masked, there ? min(t[i].mine, kend) - key - 16 * g : 0, a.c2, x[i]);
+          __builtin_amdgcn_sched_barrier(0);
+          v4i p_new[QT][3];
+          products(v);
+#pragma unroll
+          for (int i = 0; i < QT; ++i) y[i].digits(x[i], p_new[i]);
+          // one matrix instruction, then its share of the others
+#pragma unroll
+          for (int i = 0; i < 3 * NB * QT; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, (27 + NB - 1) / NB, 0);
+          }
+          __builtin_amdgcn_sched_barrier(0);
+#pragma unroll
+          for (int i = 0; i < QT; ++i)
+#pragma unroll
+            for (int j = 0; j < 3; ++j) p[i][j] = p_new[i][j];
+          if (more) transpose(v_next);
+          int8_t* const v_old = v_prev;
+          v_prev = v_cur;
+          v_cur = v_next;
+          v_next = v_old;
+        }
+        v4i v[NB];
+        values(v);
+        products(v);
+#pragma unroll
+        for (int i = 0; i < QT; ++i) y[i].fold();
+      } while (LONG && key < kend);
+    }
+#pragma unroll
+    for (int x = 0; x < QT; ++x) {
+      if (tile + x >= tiles) break;
+      y[x].sum = quad_sum(y[x].sum);
+      if (live == 1)
+        y[x].store(a, t[x], lane);
+      else
+        y[x].store_part(a.part + tile_slot(a, w, row, head, tile + x, split) * (16 * (dh + 2)), lane);
     }
   }
 }
@@ -397,42 +783,47 @@ template <int NB>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   constexpr int dh = 16 * NB;
   const int per_row = a.n_kv_heads * a.tiles;
-  const int row = blockIdx.x / per_row, head = blockIdx.x % per_row / a.tiles, tile = blockIdx.x % a.tiles;
+  const int row = blockIdx.x / per_row, head = blockIdx.x % per_row / a.tiles;
   const AttnRow w = attn_row(a, row);
-  if (16 * tile >= w.n * a.group) return;
-  const int live = live_splits(a, tile, tile_keys(a, w, tile));
-  if (live == 1) return;
-  const float* part = a.part + (size_t)blockIdx.x * a.splits * (16 * (dh + 2));
-  for (int i = threadIdx.x; i < 16 * dh / 4; i += 256) {
-    const int q = i / (dh / 4), c = 4 * (i % (dh / 4)), mq = 16 * tile + q, tq = mq / a.group;
-    if (tq >= w.n) continue;
-    float top = (float)kNoReference, wsum = 0.f;
-    float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-    for (int s = 0; s < live; ++s) top = fmaxf(top, part[(size_t)s * (16 * (dh + 2)) + 16 * dh + 16 + q]);
-    for (int s = 0; s < live; ++s) {
-      const float* src = part + (size_t)s * (16 * (dh + 2));
-      const float scale = __builtin_amdgcn_exp2f((src[16 * dh + 16 + q] - top) * a.c2);
-      const float4 x = *(const float4*)(src + q * dh + c);
-      wsum = fmaf(scale, src[16 * dh + q], wsum);
-      y.x = fmaf(scale, x.x, y.x);
-      y.y = fmaf(scale, x.y, y.y);
-      y.z = fmaf(scale, x.z, y.z);
-      y.w = fmaf(scale, x.w, y.w);
+  for (int tile = blockIdx.x % a.tiles; 16 * tile < w.n * a.group; tile += a.tiles) {
+    // a chunk's ranges go by its block's last tile
+    const int span = a.waves == 0 ? 4 * chunk_tiles(NB) : 1, last = (w.n * a.group + 15) / 16 - 1;
+    const int live = live_splits(a, tile_keys(a, w, min(tile / span * span + span - 1, last)));
+    if (live == 1) continue;
+    const float* part = a.part + tile_slot(a, w, row, head, tile, 0) * (16 * (dh + 2));
+    for (int i = threadIdx.x; i < 16 * dh / 4; i += 256) {
+      const int q = i / (dh / 4), c = 4 * (i % (dh / 4)), m = 16 * tile + q;
+      if (m / a.group >= w.n) continue;
+      float top = (float)kNoReference, sum = 0.f;
+      float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int s = 0; s < live; ++s) top = fmaxf(top, part[(size_t)s * (16 * (dh + 2)) + 16 * dh + 16 + q]);
+      for (int s = 0; s < live; ++s) {
+        const float* src = part + (size_t)s * (16 * (dh + 2));
+        const float scale = __builtin_amdgcn_exp2f((src[16 * dh + 16 + q] - top) * a.c2);
+        const float4 x = *(const float4*)(src + q * dh + c);
+        sum = fmaf(scale, src[16 * dh + q], sum);
+        y.x = fmaf(scale, x.x, y.x);
+        y.y = fmaf(scale, x.y, y.y);
+        y.z = fmaf(scale, x.z, y.z);
+        y.w = fmaf(scale, x.w, y.w);
+      }
+      store_joined(a, w, head, m, c, dh, y, sum);
     }
-    const float inv = wsum > 0.f ? a.c_pv / wsum : 0.f;
-    const size_t o = ((size_t)w.first + tq) * a.ldo + (size_t)(head * a.group + mq - tq * a.group) * dh + c;
-    if (a.kind == MNMT_ATTN_F32)
-      *(float4*)((float*)a.out + o) = make_float4(y.x * inv, y.y * inv, y.z * inv, y.w * inv);
-    else
-      *(char4*)((int8_t*)a.out + o) =
-          make_char4(code_of(y.x * inv), code_of(y.y * inv), code_of(y.z * inv), code_of(y.w * inv));
   }
 }
 
 template <int NB, bool PAGED>
-hipError_t launch_attn_nb(const AttnArgs& a, int waves, hipStream_t s) {
+hipError_t launch_attn_nb(const AttnArgs& a, hipStream_t s) {
   const int tiles = a.rows * a.n_kv_heads * a.tiles, units = tiles * a.splits;
-  if (waves == 1)
+  if (a.waves == 0)
+    hipLaunchKernelGGL((k_attn_top<NB, PAGED>), dim3(a.rows * a.n_kv_heads * (a.tiles / top_tiles(NB)) * a.splits),
+                       dim3(256), 0, s, a);
+  const dim3 chunks(a.rows * a.n_kv_heads * (a.tiles / (4 * chunk_tiles(NB))) * a.splits);
+  if (a.waves == 0 && a.cap <= kAttnKeys * kFoldSteps)
+    hipLaunchKernelGGL((k_attn_chunk<NB, PAGED, false>), chunks, dim3(256), 0, s, a);
+  else if (a.waves == 0)
+    hipLaunchKernelGGL((k_attn_chunk<NB, PAGED, true>), chunks, dim3(256), 0, s, a);
+  else if (a.waves == 1)
     hipLaunchKernelGGL((k_attn<NB, PAGED, 1>), dim3((units + 3) / 4), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((k_attn<NB, PAGED, 4>), dim3(units), dim3(256), 0, s, a);
@@ -441,16 +832,16 @@ hipError_t launch_attn_nb(const AttnArgs& a, int waves, hipStream_t s) {
 }
 
 template <bool PAGED>
-hipError_t launch_attn_kernel(const AttnArgs& a, int d_head, int waves, hipStream_t s) {
+hipError_t launch_attn_kernel(const AttnArgs& a, int d_head, hipStream_t s) {
   switch (d_head) {
-    case 16: return launch_attn_nb<1, PAGED>(a, waves, s);
-    case 32: return launch_attn_nb<2, PAGED>(a, waves, s);
-    case 48: return launch_attn_nb<3, PAGED>(a, waves, s);
-    case 64: return launch_attn_nb<4, PAGED>(a, waves, s);
-    case 80: return launch_attn_nb<5, PAGED>(a, waves, s);
-    case 96: return launch_attn_nb<6, PAGED>(a, waves, s);
-    case 112: return launch_attn_nb<7, PAGED>(a, waves, s);
-    case 128: return launch_attn_nb<8, PAGED>(a, waves, s);
+    case 16: return launch_attn_nb<1, PAGED>(a, s);
+    case 32: return launch_attn_nb<2, PAGED>(a, s);
+    case 48: return launch_attn_nb<3, PAGED>(a, s);
+    case 64: return launch_attn_nb<4, PAGED>(a, s);
+    case 80: return launch_attn_nb<5, PAGED>(a, s);
+    case 96: return launch_attn_nb<6, PAGED>(a, s);
+    case 112: return launch_attn_nb<7, PAGED>(a, s);
+    case 128: return launch_attn_nb<8, PAGED>(a, s);
     default: return hipErrorInvalidValue;
   }
 }

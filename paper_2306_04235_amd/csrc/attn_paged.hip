@@ -2,5 +2,5 @@
 #include "attention.hpp"
 
 namespace mnmt {
-template hipError_t launch_attn_kernel<true>(const AttnArgs&, int, int, hipStream_t);
+template hipError_t launch_attn_kernel<true>(const AttnArgs&, int, hipStream_t);
 }  // namespace mnmt

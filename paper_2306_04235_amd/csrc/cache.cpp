@@ -72,20 +72,22 @@ const char* attn_of(const mnmt_attn_cfg* c, int n_kv_heads, int d_head, AttnArgs
 }
 
 int run_attn(AttnArgs& a, bool paged, int d_head, int max_q, int max_len, void* d_ws, size_t ws_bytes, void* stream) {
-  const AttnPlan p = plan_attn(a.rows, a.n_kv_heads, a.group, d_head, max_q, max_len);
+  const AttnPlan p = plan_attn(a.rows, a.n, a.n_kv_heads, a.group, d_head, std::min(max_q, a.n), max_len);
   if (p.ws_bytes > ws_bytes) return bad("the workspace is smaller than mnmt_attn_ws_bytes");
   if (p.ws_bytes && (!d_ws || !aligned(d_ws, 16))) return bad("the workspace must be 16-byte aligned and not null");
   a.tiles = p.tiles;
   a.splits = p.splits;
   a.chunk = p.chunk;
+  a.waves = p.waves;
   a.part = static_cast<float*>(d_ws);
-  const hipError_t h = launch_attn(a, paged, d_head, p.waves, static_cast<hipStream_t>(stream));
+  a.tops = reinterpret_cast<int*>(static_cast<char*>(d_ws) + p.part_bytes);
+  const hipError_t h = launch_attn(a, paged, d_head, static_cast<hipStream_t>(stream));
   return h == hipSuccess ? MNMT_OK : hip_error(h, "attention launch");
 }
 
 }  // namespace
 
-AttnPlan plan_attn(int rows, int n_kv_heads, int group, int d_head, int max_q, int max_len) {
+AttnPlan plan_attn(int rows, int n, int n_kv_heads, int group, int d_head, int max_q, int max_len) {
   AttnPlan p{};
   const long heads = (long)rows * n_kv_heads;  // <= kMaxAttnUnits
   const long tiles = std::max(1L, ((long)max_q * group + 15) / 16);
@@ -94,19 +96,24 @@ AttnPlan plan_attn(int rows, int n_kv_heads, int group, int d_head, int max_q, i
   p.splits = 1;
   p.chunk = 1 << 30;
   p.waves = max_len <= 128 || units >= 2048 ? 1 : 4;
-  if (p.waves == 4 && max_len > 256 && units < 1024) {
+  if (p.tiles >= 4 && max_len > 64) {
+    p.waves = 0;
+    p.tiles = (p.tiles + 7) / 8 * 8;
+  } else if (p.waves == 4 && max_len > 256 && units < 1024) {
     const long want = std::min((1024 + units - 1) / units, (long)(max_len + 255) / 256);
     if (want > 1) {
       p.chunk = (int)((max_len + want - 1) / want + 255) / 256 * 256;
       p.splits = (max_len + p.chunk - 1) / p.chunk;
     }
   }
-  if (p.splits > 1) p.ws_bytes = (size_t)units * p.splits * 16 * (d_head + 2) * sizeof(float);
+  const size_t slots = ((size_t)n * group / 16 + rows + 1) * n_kv_heads * p.splits;  // tile_slot
+  if (p.splits > 1) p.part_bytes = slots * 16 * (d_head + 2) * sizeof(float);
+  p.ws_bytes = p.part_bytes + (p.waves == 0 ? slots * 16 * sizeof(int) : 0);
   return p;
 }
 
-hipError_t launch_attn(const AttnArgs& a, bool paged, int d_head, int waves, hipStream_t s) {
-  return paged ? launch_attn_kernel<true>(a, d_head, waves, s) : launch_attn_kernel<false>(a, d_head, waves, s);
+hipError_t launch_attn(const AttnArgs& a, bool paged, int d_head, hipStream_t s) {
+  return paged ? launch_attn_kernel<true>(a, d_head, s) : launch_attn_kernel<false>(a, d_head, s);
 }
 
 }  // namespace mnmt
@@ -203,11 +210,12 @@ extern "C" int mnmt_pages_write(const mnmt_pages_cfg* cfg, void* d_pool, int lay
   return h == hipSuccess ? MNMT_OK : hip_error(h, "write launch");
 }
 
-extern "C" size_t mnmt_attn_ws_bytes(int rows, int n_heads, int n_kv_heads, int d_head, int max_q, int max_len) {
-  if (rows < 1 || (long)rows * n_kv_heads > kMaxAttnUnits || n_kv_heads < 1 || n_kv_heads > 256 || n_heads < 1 || n_heads > 4096 ||
+extern "C" size_t mnmt_attn_ws_bytes(int rows, int n, int n_heads, int n_kv_heads, int d_head, int max_q,
+                                     int max_len) {
+  if (rows < 1 || n < 1 || n_kv_heads < 1 || (long)rows * n_kv_heads > kMaxAttnUnits || n_kv_heads > 256 || n_heads < 1 || n_heads > 4096 ||
       n_heads % n_kv_heads || d_head < 16 || d_head > 128 || d_head % 16 || max_q < 0 || max_len < 0)
     return 0;
-  return plan_attn(rows, n_kv_heads, n_heads / n_kv_heads, d_head, max_q, max_len).ws_bytes;
+  return plan_attn(rows, n, n_kv_heads, n_heads / n_kv_heads, d_head, std::min(max_q, n), max_len).ws_bytes;
 }
 
 extern "C" int mnmt_attn_paged(const mnmt_pages_cfg* pages, const mnmt_attn_cfg* cfg, const void* d_pool, int layer,

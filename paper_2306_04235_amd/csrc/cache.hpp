@@ -47,10 +47,11 @@ struct AttnArgs {
   const int32_t *start, *len;
   int n, rows, ldq, ldo, group, n_kv_heads, kind, causal;
   float c2, c_pv;  // c_qk log2 e; values' scale
-  // the launch: query tiles per row and key head in the grid, key ranges of
-  // `chunk` keys per tile, their partial results
-  int tiles, splits, chunk;
+  // the launch (AttnPlan): query tiles per row and key head in the grid, key
+  // ranges of `chunk` keys per tile, their partial results, a chunk's maxima
+  int tiles, splits, chunk, waves;
   float* part;
+  int* tops;
   // keys and values: pages of one layer, or rows [sentence][S]
   const int8_t* pool;
   const int32_t* table;
@@ -61,15 +62,15 @@ struct AttnArgs {
   int cap;  // longest length
 };
 
-// Fills the launch fields from the caller's bounds (host only) and returns the
-// workspace that the call needs.
+// The launch of a call, by the caller's bounds, and the workspace that it needs.
 struct AttnPlan {
-  int tiles, splits, chunk, waves;  // waves per query tile: 1 or 4
-  size_t ws_bytes;
+  int tiles, splits, chunk;
+  int waves;  // per query tile: 1 or 4; 0: the chunk kernels
+  size_t part_bytes, ws_bytes;
 };
-AttnPlan plan_attn(int rows, int n_kv_heads, int group, int d_head, int max_q, int max_len);
-hipError_t launch_attn(const AttnArgs& a, bool paged, int d_head, int waves, hipStream_t s);
+AttnPlan plan_attn(int rows, int n, int n_kv_heads, int group, int d_head, int max_q, int max_len);
+hipError_t launch_attn(const AttnArgs& a, bool paged, int d_head, hipStream_t s);
 template <bool PAGED>
-hipError_t launch_attn_kernel(const AttnArgs& a, int d_head, int waves, hipStream_t s);
+hipError_t launch_attn_kernel(const AttnArgs& a, int d_head, hipStream_t s);
 
 }  // namespace mnmt

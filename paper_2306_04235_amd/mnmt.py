@@ -110,7 +110,7 @@ def lib():
         L.mnmt_pages_fork.argtypes = [pages, vp, vp, vp, i32, vp, vp, i32, vp, vp, vp, vp, sz, vp]
         L.mnmt_pages_compact.argtypes = [pages, vp, vp, vp, i32, vp, vp, vp, sz, vp]
         L.mnmt_pages_write.argtypes = [pages, vp, i32, vp, vp, i32, vp, vp, i64, vp, i32, i32, vp]
-        L.mnmt_attn_ws_bytes.argtypes = [i32, i32, i32, i32, i32, i32]
+        L.mnmt_attn_ws_bytes.argtypes = [i32] * 7
         L.mnmt_attn_ws_bytes.restype = sz
         L.mnmt_attn_paged.argtypes = [pages, attn, vp, i32, vp, vp, i32, vp, vp, i32, vp, vp, sz, vp]
         L.mnmt_attn_cross.argtypes = [attn, i32, i32, vp, vp, i64, i64, i32, vp, i32, vp, vp, i32, vp, vp, sz, vp]
@@ -315,11 +315,11 @@ def _pages(pool_shape, width: int, rows: int):
 
 
 @functools.lru_cache(maxsize=256)
-def _attn(rows, hkv, dh, d, kind, causal, ld, ldo, most, longest, c_qk, c_pv):
+def _attn(rows, n, hkv, dh, d, kind, causal, ld, ldo, most, longest, c_qk, c_pv):
     """An attention call's configuration and workspace."""
     _need(dh > 0 and d > 0 and d % dh == 0, "q must have whole heads")
     a = AttnCfg(d // dh, kind, causal, ld, ldo, most, longest, c_qk, c_pv)
-    return C.byref(a), lib().mnmt_attn_ws_bytes(rows, d // dh, hkv, dh, most, longest)
+    return C.byref(a), lib().mnmt_attn_ws_bytes(rows, n, d // dh, hkv, dh, most, longest)
 
 
 def _need(ok, what):
@@ -495,7 +495,7 @@ def mnmt_attn_paged(q, pool, layer, table, lens, c_qk, c_pv, kind=ATTN_F32, star
     _device(pool)
     out, ldo = _attn_out(q, kind, out)
     longest = width * shape.page_size
-    a, nbytes = _attn(rows, shape.n_kv_heads, shape.d_head, d, kind, 1 if causal else 0, ld, ldo,
+    a, nbytes = _attn(rows, n, shape.n_kv_heads, shape.d_head, d, kind, 1 if causal else 0, ld, ldo,
                       _most(n, rows, start, max_q), longest if max_len is None else min(max_len, longest), c_qk, c_pv)
     ws = _workspace(nbytes, q, stream) if nbytes else None
     rc = _lib.mnmt_attn_paged(cfg, a, pool.data_ptr(), layer, table.data_ptr(), lens.data_ptr(), rows, q.data_ptr(),
@@ -526,7 +526,7 @@ def mnmt_attn_cross(q, k, v, lens, d_head, c_qk, c_pv, kind=ATTN_F32, start=None
     _device(q)
     out, ldo = _attn_out(q, kind, out)
     hkv = width // d_head
-    a, nbytes = _attn(rows, hkv, d_head, d, kind, 0, ldq, ldo, _most(n, rows, start, max_q), S, c_qk, c_pv)
+    a, nbytes = _attn(rows, n, hkv, d_head, d, kind, 0, ldq, ldo, _most(n, rows, start, max_q), S, c_qk, c_pv)
     ws = _workspace(nbytes, q, stream) if nbytes else None
     rc = _lib.mnmt_attn_cross(a, hkv, d_head, k.data_ptr(), v.data_ptr(), ld if S > 1 else width, batch if rows > 1 else 0,
                               S, lens.data_ptr(), rows, q.data_ptr(), _ptr(start), n, out.data_ptr(), _ptr(ws), nbytes,

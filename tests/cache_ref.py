@@ -130,12 +130,12 @@ def paged(cache, layer, table, lens, q, start, h, c_qk, c_pv, causal=True):
 
 def tolerance(share, c_pv):
     """How far an attention output may be from float64; share: keys over the sum of the weights, the largest one being 1.
-    A weight is a fixed-point number of unit 2^-22.99 of the largest weight so far, which is at most the largest: half
+    A weight is a fixed-point number of unit 1 / 0x7F7F7F of the largest weight so far, which is at most the largest: half
     a unit for each key, times |v| <= 128 in the numerator and as much again through the denominator, over the sum.  The
     exponential: its argument rounds by 2^-24 of at most 24 (smaller weights vanish), times ln 2, plus 2^-23 for the
     exponential itself and 2^-24 for c_qk: 1.2e-6 of each weight, in the numerator and the denominator; the sums, the
     joins and the division in fp32 are 8 roundings more."""
-    return abs(c_pv) * 128.0 * (share * 2.0 ** -22.99 + 2.4e-6 + 8 * 2.0 ** -24)
+    return abs(c_pv) * 128.0 * (share / 0x7F7F7F + 2.4e-6 + 8 * 2.0 ** -24)
 
 
 def check_codes(got, ref, tol):

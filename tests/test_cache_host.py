@@ -44,10 +44,11 @@ def test_sizes():
         assert L.mnmt_pages_bytes(C.byref(pages(**kw))) == 0, kw
         assert L.mnmt_pages_ws_bytes(C.byref(pages(**kw)), 1) == 0, kw
     assert L.mnmt_pages_bytes(None) == 0
-    assert L.mnmt_attn_ws_bytes(4, 8, 8, 64, 1, 40) == 0      # one pass
-    assert L.mnmt_attn_ws_bytes(1, 8, 8, 64, 1, 30000) > 0    # joined ranges
-    for args in ((0, 8, 8, 64, 1, 9), (1, 9, 8, 64, 1, 9), (1, 8, 8, 65, 1, 9), (1, 8, 8, 64, -1, 9),
-                 (1, 8, 8, 64, 1, -1), (1, 0, 1, 64, 1, 9), (1, 8, 0, 64, 1, 9)):
+    assert L.mnmt_attn_ws_bytes(4, 4, 8, 8, 64, 1, 40) == 0      # one pass
+    assert L.mnmt_attn_ws_bytes(1, 1, 8, 8, 64, 1, 30000) > 0    # joined ranges
+    big = 1 << 20
+    for args in ((0, 1, 8, 8, 64, 1, big), (1, 0, 8, 8, 64, 1, big), (1, 1, 9, 8, 64, 1, big), (1, 1, 8, 8, 65, 1, big),
+                 (1, 1, 8, 8, 64, -1, big), (1, 1, 8, 8, 64, 1, -1), (1, 1, 0, 1, 64, 1, big), (1, 1, 8, 0, 64, 1, big)):
         assert L.mnmt_attn_ws_bytes(*args) == 0, args
 
 
