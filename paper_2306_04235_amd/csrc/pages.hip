@@ -46,28 +46,56 @@ __device__ __forceinline__ int page_at(const PagesShape& s, const int32_t* table
   return p < 0 || p >= s.n_pages ? -1 : p;
 }
 
+// What the plans know of a page, in `first`: kShared if a row shares it, else the
+// lowest row that is to write to it, else kFree.
+constexpr int kShared = -1, kFree = INT_MAX;
+
 __global__ __launch_bounds__(256) void k_pages_clear(int* first, int n) {
-  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) first[i] = INT_MAX;
+  for (int i = blockIdx.x * 256 + threadIdx.x; i < n; i += gridDim.x * 256) first[i] = kFree;
 }
 
-// first[p] = -1 if a row shares page p, else the lowest row that is to write to
-// it, else INT_MAX (free).  One block per row.
-__global__ __launch_bounds__(64) void k_fork_mark(PagesFork f, int* first) {
-  const int r = blockIdx.x;
+// Marks an output row's pages; thread `t` of `step`.  Sharing wins whichever
+// comes first.
+template <class Share, class Write>
+__device__ __forceinline__ void mark_row(const PagesFork& f, int r, int t, int step, Share share, Write write) {
   const RowPlan p = plan_row(f, r);
   if (p.parent < 0) return;
-  for (int c = threadIdx.x; c < p.old; c += 64) {
-    const int page = page_at(f.s, f.table, p.parent, c);
-    if (page >= 0) atomicMin(&first[page], c < p.whole ? -1 : r);
+  constexpr int U = 4;  // loads under way at once
+  for (int c0 = t; c0 < p.old; c0 += U * step) {
+    int page[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) page[u] = c0 + u * step < p.old ? page_at(f.s, f.table, p.parent, c0 + u * step) : -1;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (page[u] < 0) continue;
+      if (c0 + u * step < p.whole)
+        share(page[u]);
+      else
+        write(page[u]);
+    }
   }
 }
 
-__global__ __launch_bounds__(64) void k_compact_mark(PagesFork f, int* first) {
-  const int r = blockIdx.x, n = plan_row(f, r).old;
-  for (int c = threadIdx.x; c < n; c += 64) {
-    const int page = page_at(f.s, f.table, r, c);
-    if (page >= 0) first[page] = -1;
-  }
+// Rows next to each other often share most of their pages (samples of one
+// prompt): a block of 16 rows notes in LDS which of the pages it has marked
+// (2048 rows of 63-126 pages, 32 rows to a prompt: 17 us without).
+constexpr int kMarkRows = 16, kMarkBits = 1 << 18;
+
+__global__ __launch_bounds__(1024) void k_pages_mark(PagesFork f, int* first) {
+  __shared__ uint32_t seen[kMarkBits / 32];
+  const int words = f.s.n_pages <= kMarkBits ? (f.s.n_pages + 31) / 32 : 0;
+  for (int i = threadIdx.x; i < words; i += 1024) seen[i] = 0;
+  __syncthreads();
+  const int r = blockIdx.x * kMarkRows + (threadIdx.x >> 6);
+  if (r >= f.rows) return;
+  mark_row(
+      f, r, threadIdx.x & 63, 64,
+      [&](int page) {
+        const uint32_t bit = 1u << (page & 31);
+        if (words == 0 || !(atomicOr(&seen[page >> 5], bit) & bit))
+          __hip_atomic_store(&first[page], kShared, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+      },
+      [&](int page) { atomicMin(&first[page], r); });
 }
 
 // Exclusive prefix sum of one value per thread of a 1024-thread block; *total
@@ -94,42 +122,156 @@ __device__ __forceinline__ int block_scan(int v, int* total) {
   return before + x - v;
 }
 
-// Rows' places in the list of free pages, and the list (one block).
-__global__ __launch_bounds__(1024) void k_fork_plan(PagesFork f, const int* first, int* place, int* source, int* list,
-                                                    int32_t* info) {
-  const int tid = threadIdx.x;
-  long want = 0;  // pages wanted by the rows before
-  for (int r0 = 0; r0 < f.rows; r0 += 1024) {
-    const int r = r0 + tid;
-    int n = 0, src = -1;
-    if (r < f.rows) {
-      const RowPlan p = plan_row(f, r);
-      if (p.old > p.whole) {
-        src = page_at(f.s, f.table, p.parent, p.whole);
-        if (src >= 0 && first[src] == r) src = -1;  // its own
+// take(i, k) for the k-th i in lo..n-1 with is(at(i)), in order; how many there
+// are.  A wave has a range of its own and goes over it twice, 256 values at a time
+// (at4(i): four from i on, i a multiple of 4): no barrier between the steps.  Every
+// thread of a 1024-thread block calls it.
+template <class At4, class Is, class Take>
+__device__ __forceinline__ int block_list(int lo, int n, At4 at4, Is is, Take take) {
+  __shared__ int wsum[16];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, from = lo & ~3;
+  const int span = (max(n - from, 0) + 4095) / 4096 * 256, begin = from + wave * span, end = min(begin + span, n);
+  const unsigned long long below = (1ull << lane) - 1;
+  auto look = [&](int i, bool (&it)[4]) {
+    const int at = i + 4 * lane;
+    const int4 x = at < end ? at4(at) : make_int4(0, 0, 0, 0);
+    it[0] = at >= lo && at < end && is(x.x);
+    it[1] = at + 1 >= lo && at + 1 < end && is(x.y);
+    it[2] = at + 2 >= lo && at + 2 < end && is(x.z);
+    it[3] = at + 3 >= lo && at + 3 < end && is(x.w);
+  };
+  int count = 0;
+#pragma unroll 4
+  for (int i = begin; i < end; i += 256) {
+    bool it[4];
+    look(i, it);
+#pragma unroll
+    for (int u = 0; u < 4; ++u) count += __popcll(__ballot(it[u]));
+  }
+  __syncthreads();
+  if (lane == 0) wsum[wave] = count;
+  __syncthreads();
+  int before = 0, all = 0;
+#pragma unroll
+  for (int w = 0; w < 16; ++w) {
+    if (w < wave) before += wsum[w];
+    all += wsum[w];
+  }
+#pragma unroll 4
+  for (int i = begin; i < end; i += 256) {
+    bool it[4];
+    look(i, it);
+    int k = before;
+#pragma unroll
+    for (int u = 0; u < 4; ++u) {
+      const unsigned long long b = __ballot(it[u]);
+      k += __popcll(b & below);
+      before += __popcll(b);
+    }
+#pragma unroll
+    for (int u = 0; u < 4; ++u)
+      if (it[u]) take(i + 4 * lane + u, k++);
+  }
+  return all;
+}
+
+// Rows' places in the list of free pages; places[rows + 1]: pages wanted in all.
+template <class At>
+__device__ __forceinline__ void plan_rows(const PagesFork& f, At at, int* place, int* source) {
+  constexpr int U = 4;  // rows of a thread
+  long want = 0;        // pages wanted by the rows before
+  for (int r0 = 0; r0 < f.rows; r0 += 1024 * U) {
+    int n[U], src[U], sum = 0;
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + U * threadIdx.x + u;
+      n[u] = 0;
+      src[u] = -1;
+      if (r < f.rows) {
+        const RowPlan p = plan_row(f, r);
+        if (p.old > p.whole) src[u] = page_at(f.s, f.table, p.parent, p.whole);
+        n[u] = p.pages - p.old;
       }
-      n = p.pages - p.old + (src >= 0);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      if (src[u] >= 0 && at(src[u]) == r0 + U * (int)threadIdx.x + u) src[u] = -1;  // its own
+      n[u] += src[u] >= 0;
+      sum += n[u];
     }
     int all;
-    const int at = block_scan(n, &all);
-    if (r < f.rows) {
-      place[r] = clamped(want + at, 0, INT_MAX);
-      source[r] = src;
+    int k = block_scan(sum, &all);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + U * threadIdx.x + u;
+      if (r < f.rows) {
+        place[r] = clamped(want + k, 0, INT_MAX);
+        source[r] = src[u];
+      }
+      k += n[u];
     }
     want += all;
   }
-  long free_pages = 0;
-  for (int p0 = 0; p0 < f.s.n_pages; p0 += 1024) {
-    const int p = p0 + tid, is_free = p < f.s.n_pages && first[p] == INT_MAX;
-    int all;
-    const int at = block_scan(is_free, &all);
-    if (is_free) list[free_pages + at] = p;
-    free_pages += all;
+  if (threadIdx.x == 0) place[f.rows + 1] = clamped(want, 0, INT_MAX);
+}
+
+// The free pages in order; places[rows]: how many there are.
+template <class At4>
+__device__ __forceinline__ void plan_free(const PagesFork& f, At4 at4, int* place, int* list) {
+  const int n = block_list(0, f.s.n_pages, at4, [](int x) { return x == kFree; }, [&](int p, int k) { list[k] = p; });
+  if (threadIdx.x == 0) place[f.rows] = n;
+}
+
+// to[p]: where page p goes, -1 where it is free (one block).
+template <class At4>
+__device__ __forceinline__ void compact_plan(const PagesFork& f, At4 at4, int* to, int* list, int32_t* info) {
+  const int n = f.s.n_pages;
+  for (int p = threadIdx.x; p < n; p += 1024) to[p] = -1;
+  __syncthreads();
+  auto used = [](int x) { return x != kFree; };
+  const int live = block_list(0, n, at4, used, [&](int p, int) { to[p] = p; });
+  block_list(0, live, at4, [](int x) { return x == kFree; }, [&](int p, int k) { list[k] = p; });
+  __syncthreads();
+  const int moved = block_list(live, n, at4, used, [&](int p, int k) { to[p] = list[k]; });
+  if (threadIdx.x == 0) {
+    info[0] = live;
+    info[1] = moved;
   }
-  if (tid == 0) {
-    info[0] = clamped(free_pages - want, 0, INT_MAX);
-    info[1] = clamped(want - free_pages, 0, INT_MAX);
-    place[f.rows] = (int)free_pages;
+}
+
+// Block 0: the rows, block 1: the free pages.
+__global__ __launch_bounds__(1024) void k_fork_plan(PagesFork f, const int* first, int* place, int* source, int* list) {
+  if (blockIdx.x == 0)
+    plan_rows(f, [&](int p) { return first[p]; }, place, source);
+  else
+    plan_free(f, [&](int p) { return *(const int4*)(first + p); }, place, list);
+}
+__global__ __launch_bounds__(1024) void k_compact_plan(PagesFork f, const int* first, int* to, int* list,
+                                                       int32_t* info) {
+  compact_plan(f, [&](int p) { return *(const int4*)(first + p); }, to, list, info);
+}
+
+// Small caches: marks and plan in one launch, the marks in LDS.
+constexpr int kSmallPages = 12288, kSmallEntries = 32768;
+
+template <bool COMPACT>
+__global__ __launch_bounds__(1024) void k_pages_small(PagesFork f, int* place, int* source, int* list, int32_t* info) {
+  __shared__ __attribute__((aligned(16))) int first[kSmallPages];
+  for (int i = threadIdx.x; i < f.s.n_pages; i += 1024) first[i] = kFree;
+  __syncthreads();
+  int per = 1;  // threads of a row: all rows at once, if there are so few
+  while (per < 64 && 2 * per * f.rows <= 1024) per *= 2;
+  for (int r = threadIdx.x / per; r < f.rows; r += 1024 / per)
+    mark_row(
+        f, r, threadIdx.x % per, per, [&](int page) { first[page] = kShared; },
+        [&](int page) { atomicMin(&first[page], r); });
+  __syncthreads();
+  auto at4 = [&](int p) { return *(const int4*)(first + p); };
+  if (COMPACT) {
+    compact_plan(f, at4, place, list, info);
+  } else {
+    plan_rows(f, [&](int p) { return first[p]; }, place, source);
+    plan_free(f, at4, place, list);
   }
 }
 
@@ -154,13 +296,18 @@ __device__ __forceinline__ void copy_chunk(const PagesShape& s, int8_t* pool, in
 }
 
 __global__ __launch_bounds__(256) void k_fork_apply(PagesFork f, const int* place, const int* source, const int* list,
-                                                    const int32_t* info, int32_t* table_out, int32_t* len_out) {
-  const int r = blockIdx.x, src = source[r], free_pages = place[f.rows];
-  int at = place[r];
+                                                    int32_t* table_out, int32_t* len_out, int32_t* info) {
+  const int r = blockIdx.x, src = r < f.rows ? source[r] : -1, free_pages = place[f.rows], want = place[f.rows + 1];
+  const int at = r < f.rows ? place[r] : 0;
   if (blockIdx.y > 0) {  // nothing is copied where pages are missing: the input tables still hold
-    if (src >= 0 && info[1] == 0) copy_chunk(f.s, f.pool, src, list[at], blockIdx.y - 1);
+    if (src >= 0 && want <= free_pages) copy_chunk(f.s, f.pool, src, list[at], blockIdx.y - 1);
     return;
   }
+  if (r == 0 && threadIdx.x == 0) {
+    info[0] = max(free_pages - want, 0);
+    info[1] = max(want - free_pages, 0);
+  }
+  if (r >= f.rows) return;  // (there are no rows: only the counts)
   const RowPlan p = plan_row(f, r);
   __syncthreads();  // the row is planned by every wave before its length is written (they may be the same array)
   if (threadIdx.x == 0) len_out[r] = p.len;
@@ -177,51 +324,25 @@ __global__ __launch_bounds__(256) void k_fork_apply(PagesFork f, const int* plac
   }
 }
 
-// to[p]: where page p goes.  One block.
-__global__ __launch_bounds__(1024) void k_compact_plan(PagesFork f, const int* first, int* to, int* list,
-                                                       int32_t* info) {
-  const int tid = threadIdx.x, n = f.s.n_pages;
-  int live = 0;
-  for (int p0 = 0; p0 < n; p0 += 1024) {
-    int all;
-    block_scan(p0 + tid < n && first[p0 + tid] < 0, &all);
-    live += all;
+// Block row 0: the table's new numbers, a row per block; the others: one chunk of
+// a page of one layer, a page per block.
+__global__ __launch_bounds__(256) void k_compact_apply(PagesFork f, const int* to, const int32_t* info,
+                                                       int32_t* table_out) {
+  if (blockIdx.y > 0) {
+    // only the pages from info[0] on move
+    const int p = blockIdx.x + info[0];
+    if (p >= f.s.n_pages) return;
+    const int q = to[p];
+    if (q >= 0) copy_chunk(f.s, f.pool, p, q, blockIdx.y - 1);
+    return;
   }
-  int holes = 0;
-  for (int p0 = 0; p0 < live; p0 += 1024) {
-    const int p = p0 + tid, hole = p < live && first[p] >= 0;
-    int all;
-    const int at = block_scan(hole, &all);
-    if (hole) list[holes + at] = p;
-    if (p < live) to[p] = p;
-    holes += all;
+  for (int r = blockIdx.x; r < f.rows; r += gridDim.x) {
+    const int n = plan_row(f, r).old;
+    for (int c = threadIdx.x; c < f.s.max_pages; c += 256) {
+      const int page = c < n ? page_at(f.s, f.table, r, c) : -1;
+      table_out[(size_t)r * f.s.max_pages + c] = page < 0 ? -1 : to[page];
+    }
   }
-  __syncthreads();
-  int moved = 0;
-  for (int p0 = live; p0 < n; p0 += 1024) {
-    const int p = p0 + tid, high = p < n && first[p] < 0;
-    int all;
-    const int at = block_scan(high, &all);
-    if (p < n) to[p] = high ? list[moved + at] : p;
-    moved += all;
-  }
-  if (tid == 0) {
-    info[0] = live;
-    info[1] = moved;
-  }
-}
-
-__global__ __launch_bounds__(256) void k_compact_table(PagesFork f, const int* to, int32_t* table_out) {
-  const int r = blockIdx.x, n = plan_row(f, r).old;
-  for (int c = threadIdx.x; c < f.s.max_pages; c += 256) {
-    const int page = c < n ? page_at(f.s, f.table, r, c) : -1;
-    table_out[(size_t)r * f.s.max_pages + c] = page < 0 ? -1 : to[page];
-  }
-}
-
-__global__ __launch_bounds__(256) void k_compact_move(PagesFork f, const int* to) {
-  const int p = blockIdx.x, q = to[p];
-  if (q != p) copy_chunk(f.s, f.pool, p, q, blockIdx.y);
 }
 
 // Codes of new tokens into their pages: one block per group of 16 tokens and
@@ -292,7 +413,7 @@ PagesWs split_ws(const PagesShape& s, int rows, void* ws) {
   w.first = static_cast<int*>(ws);
   w.list = w.first + s.n_pages;
   w.place = w.list + s.n_pages;
-  w.source = w.place + rows + 1;
+  w.source = w.place + rows + 2;
   return w;
 }
 
@@ -305,30 +426,48 @@ int pages_copy_parts(const PagesShape& s) {
 }
 
 size_t pages_ws_bytes(const PagesShape& s, int rows) {
-  return sizeof(int) * (3 * (size_t)s.n_pages + 2 * (size_t)rows + 1);
+  return sizeof(int) * (3 * (size_t)s.n_pages + 2 * (size_t)rows + 2);
+}
+
+// Whether one block marks and plans.  One CU then reads the whole table, which is
+// soon done for a beam's (512 rows of 6 entries: 6 us for the launch instead of 12
+// for three), but not for long rows of many (2048 of 126).
+static bool small_cache(const PagesFork& f) {
+  return f.s.n_pages <= kSmallPages && (long)f.rows * f.s.max_pages <= kSmallEntries;
+}
+
+static void mark_pages(const PagesFork& f, int* first, hipStream_t s) {
+  hipLaunchKernelGGL(k_pages_clear, dim3(clear_blocks(f.s.n_pages)), dim3(256), 0, s, first, f.s.n_pages);
+  if (f.rows > 0)
+    hipLaunchKernelGGL(k_pages_mark, dim3((f.rows + kMarkRows - 1) / kMarkRows), dim3(1024), 0, s, f, first);
 }
 
 hipError_t launch_pages_fork(const PagesFork& f, int32_t* table_out, int32_t* len_out, int32_t* info, void* ws,
                              hipStream_t s) {
   const PagesWs w = split_ws(f.s, f.rows, ws);
-  hipLaunchKernelGGL(k_pages_clear, dim3(clear_blocks(f.s.n_pages)), dim3(256), 0, s, w.first, f.s.n_pages);
-  if (f.rows > 0) hipLaunchKernelGGL(k_fork_mark, dim3(f.rows), dim3(64), 0, s, f, w.first);
-  hipLaunchKernelGGL(k_fork_plan, dim3(1), dim3(1024), 0, s, f, w.first, w.place, w.source, w.list, info);
-  if (f.rows > 0)
-    hipLaunchKernelGGL(k_fork_apply, dim3(f.rows, 1 + pages_copy_parts(f.s)), dim3(256), 0, s, f, w.place, w.source,
-                       w.list, info, table_out, len_out);
+  if (small_cache(f)) {
+    hipLaunchKernelGGL(k_pages_small<false>, dim3(1), dim3(1024), 0, s, f, w.place, w.source, w.list, info);
+  } else {
+    mark_pages(f, w.first, s);
+    hipLaunchKernelGGL(k_fork_plan, dim3(2), dim3(1024), 0, s, f, w.first, w.place, w.source, w.list);
+  }
+  hipLaunchKernelGGL(k_fork_apply, dim3(std::max(f.rows, 1), 1 + pages_copy_parts(f.s)), dim3(256), 0, s, f, w.place,
+                     w.source, w.list, table_out, len_out, info);
   return hipGetLastError();
 }
 
 hipError_t launch_pages_compact(const PagesFork& f, int32_t* table_out, int32_t* info, void* ws, hipStream_t s) {
   const PagesWs w = split_ws(f.s, 0, ws);
   int* to = w.place;
-  hipLaunchKernelGGL(k_pages_clear, dim3(clear_blocks(f.s.n_pages)), dim3(256), 0, s, w.first, f.s.n_pages);
-  if (f.rows > 0) hipLaunchKernelGGL(k_compact_mark, dim3(f.rows), dim3(64), 0, s, f, w.first);
-  hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(1024), 0, s, f, w.first, to, w.list, info);
-  if (f.rows == 0) return hipGetLastError();
-  hipLaunchKernelGGL(k_compact_table, dim3(f.rows), dim3(256), 0, s, f, to, table_out);
-  hipLaunchKernelGGL(k_compact_move, dim3(f.s.n_pages, pages_copy_parts(f.s)), dim3(256), 0, s, f, to);
+  if (small_cache(f)) {
+    hipLaunchKernelGGL(k_pages_small<true>, dim3(1), dim3(1024), 0, s, f, to, nullptr, w.list, info);
+  } else {
+    mark_pages(f, w.first, s);
+    hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(1024), 0, s, f, w.first, to, w.list, info);
+  }
+  if (f.rows > 0)
+    hipLaunchKernelGGL(k_compact_apply, dim3(f.s.n_pages, 1 + pages_copy_parts(f.s)), dim3(256), 0, s, f, to, info,
+                       table_out);
   return hipGetLastError();
 }
 
