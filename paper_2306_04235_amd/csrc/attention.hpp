@@ -19,10 +19,8 @@
 // An error of half a unit is 2^-24 of a row's largest weight, so that the
 // softmax is fp32 throughout in effect, and the sums do not depend on order.
 //
-// One pass: scores are taken relative to the largest so far, an int32 that starts
-// the products' accumulators at its negative for nothing.  Where a step brings a
-// larger one, the sums so far are folded into fp32 and rescaled; the other steps
-// (after a row's first keys, most) add integers only.
+// Scores are taken relative to the largest so far (steps) or of all (chunks), an
+// int32 that starts the products' accumulators at its negative for nothing.
 #pragma once
 
 #include <climits>
@@ -162,129 +160,86 @@ struct TileQuery {
   }
 };
 
-// The sums of a query tile: columns 16 b + 4 (lane / 16) + i of query lane % 16.
-template <int NB>
-struct TileSums {
-  v4i acc[3][NB];  // digits' products since the last fold
-  float f[NB][4], sum;
-  int ref, steps;
-  bool folded;
-
-  __device__ __forceinline__ TileSums() : sum(0.f), ref(kNoReference), steps(0), folded(false) {
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f[b][i] = 0.f;
-        acc[0][b][i] = acc[1][b][i] = acc[2][b][i] = 0;
-      }
-  }
-  __device__ __forceinline__ void fold() {
-#pragma unroll
-    for (int b = 0; b < NB; ++b)
-#pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        f[b][i] = fmaf(65536.f, (float)acc[0][b][i], f[b][i]);
-        f[b][i] = fmaf(256.f, (float)acc[1][b][i], f[b][i]);
-        f[b][i] += (float)acc[2][b][i];
-        acc[0][b][i] = acc[1][b][i] = acc[2][b][i] = 0;
-      }
-  }
-  // The lane's largest; what is masked becomes INT_MIN / 2.
-  static __device__ __forceinline__ int largest(v4i (&d)[4], bool masked, int count) {
-    if (masked) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          int v = 4 * j + i >= count ? INT_MIN / 2 : d[j][i];
-          asm volatile("" : "+v"(v));  // (stays in this branch: as a select it would cost every step)
-          d[j][i] = v;
-        }
-    }
-    int top = max(max(d[0][0], d[0][1]), d[0][2]);
-    top = max(top, d[0][3]);
-#pragma unroll
-    for (int j = 1; j < 4; ++j) {
-      top = max(max(top, d[j][0]), d[j][1]);
-      top = max(max(top, d[j][2]), d[j][3]);
-    }
-    return top;
-  }
-  // Weights of a step: d[j][i] = score less ref of the lane's query and key 4 j + i
-  // of its 16, of which the first `count` are seen (all where not masked); p: the
-  // weights' digits.
-  __device__ __forceinline__ void weigh(v4i (&d)[4], bool masked, int count, float c2, v4i (&p)[3]) {
-    int top = quad_max(largest(d, masked, count));
-    ++steps;
-    if (__any(top > 0) || steps == kFoldSteps) {
-      const int up = max(top, 0);
-      if (steps > 1 || folded) {
-        const float scale = __builtin_amdgcn_exp2f(-(float)up * c2);
-        fold();
-        folded = true;
-        steps = 1;
-#pragma unroll
-        for (int b = 0; b < NB; ++b)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) f[b][i] *= scale;
-        sum *= scale;
-      }
-      ref += up;
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) d[j][i] -= up;  // (masked places stay far below)
-    }
-    float x[4][4];
-    exponents(d, masked, count, c2, x);
-    digits(x, p);
-  }
-  // Exponents c2 d; -inf where masked.
-  static __device__ __forceinline__ void exponents(const v4i (&d)[4], bool masked, int count, float c2,
-                                                   float (&x)[4][4]) {
+// The lane's largest of a step's scores; d[j][i]: its query and key 4 j + i of its
+// 16, of which the first `count` are seen (all where not masked).
+__device__ __forceinline__ int largest(v4i (&d)[4], bool masked, int count) {
+  if (masked) {
 #pragma unroll
     for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) x[j][i] = (float)d[j][i] * c2;
-    if (masked) {
-#pragma unroll
-      for (int j = 0; j < 4; ++j)
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          x[j][i] = 4 * j + i >= count ? -__builtin_inff() : x[j][i];
-          asm volatile("" : "+v"(x[j][i]));
-        }
-    }
+      for (int i = 0; i < 4; ++i) {
+        int v = 4 * j + i >= count ? INT_MIN / 2 : d[j][i];
+        asm volatile("" : "+v"(v));  // (stays in this branch: as a select it would cost every step)
+        d[j][i] = v;
+      }
   }
-  // Digits of the weights 2^x.
-  __device__ __forceinline__ void digits(const float (&x)[4][4], v4i (&p)[3]) {
-    uint32_t total = 0;
+  int top = max(max(d[0][0], d[0][1]), d[0][2]);
+  top = max(top, d[0][3]);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      uint32_t u[4];
+  for (int j = 1; j < 4; ++j) {
+    top = max(max(top, d[j][0]), d[j][1]);
+    top = max(max(top, d[j][2]), d[j][3]);
+  }
+  return top;
+}
+
+// Exponents c2 d; -inf where masked.
+__device__ __forceinline__ void exponents(const v4i (&d)[4], bool masked, int count, float c2, float (&x)[4][4]) {
+#pragma unroll
+  for (int j = 0; j < 4; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) x[j][i] = (float)d[j][i] * c2;
+  if (masked) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        u[i] = __float_as_uint(fmaf(__builtin_amdgcn_exp2f(x[j][i]), kOne, kDigits));
-        total += u[i];
+        x[j][i] = 4 * j + i >= count ? -__builtin_inff() : x[j][i];
+        asm volatile("" : "+v"(x[j][i]));
       }
-      const uint32_t lo0 = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
-      const uint32_t hi0 = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0602u), hi1 = __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0602u);
-      p[0][j] = (int)__builtin_amdgcn_perm(hi1, hi0, 0x05040100u);
-      p[1][j] = (int)(__builtin_amdgcn_perm(lo1, lo0, 0x07060302u) ^ 0x80808080u);
-      p[2][j] = (int)(__builtin_amdgcn_perm(lo1, lo0, 0x05040100u) ^ 0x80808080u);
-    }
-    sum += (float)(total - 16u * kDigitBits);
   }
-  __device__ __forceinline__ void add(int b, v4i values, const v4i (&p)[3]) {
+}
+
+// Digits of the weights 2^x; returns the weights' sum.
+__device__ __forceinline__ float digits(const float (&x)[4][4], v4i (&p)[3]) {
+  uint32_t total = 0;
 #pragma unroll
-    for (int x = 0; x < 3; ++x) acc[x][b] = mfma16(values, p[x], acc[x][b]);
+  for (int j = 0; j < 4; ++j) {
+    uint32_t u[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      u[i] = __float_as_uint(fmaf(__builtin_amdgcn_exp2f(x[j][i]), kOne, kDigits));
+      total += u[i];
+    }
+    const uint32_t lo0 = __builtin_amdgcn_perm(u[1], u[0], 0x05010400u), lo1 = __builtin_amdgcn_perm(u[3], u[2], 0x05010400u);
+    const uint32_t hi0 = __builtin_amdgcn_perm(u[1], u[0], 0x0c0c0602u), hi1 = __builtin_amdgcn_perm(u[3], u[2], 0x0c0c0602u);
+    p[0][j] = (int)__builtin_amdgcn_perm(hi1, hi0, 0x05040100u);
+    p[1][j] = (int)(__builtin_amdgcn_perm(lo1, lo0, 0x07060302u) ^ 0x80808080u);
+    p[2][j] = (int)(__builtin_amdgcn_perm(lo1, lo0, 0x05040100u) ^ 0x80808080u);
+  }
+  return (float)(total - 16u * kDigitBits);
+}
+
+// The sums of a query tile: columns 16 b + 4 (lane / 16) + i of query lane % 16,
+// relative to the weight of score ref.
+template <int NB>
+struct TileSums {
+  float f[NB][4], sum;
+  int ref;
+
+  __device__ __forceinline__ TileSums() : sum(0.f), ref(kNoReference) {
+#pragma unroll
+    for (int b = 0; b < NB; ++b)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) f[b][i] = 0.f;
+  }
+  // f scale + the digits' products a, b, c
+  __device__ __forceinline__ void fold(int block, float scale, v4i a, v4i b, v4i c) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      f[block][i] = fmaf(65536.f, (float)a[i], fmaf(256.f, (float)b[i], fmaf(f[block][i], scale, (float)c[i])));
   }
   // After the last step: the query's outputs, or its partial result [16][dh], sums [16], references [16].
-  __device__ __forceinline__ void close() {
-    fold();
-    sum = quad_sum(sum);
-  }
   __device__ __forceinline__ void store(const AttnArgs& a, const TileQuery<NB>& t, int lane) const {
     if (!t.real) return;
     const float inv = sum > 0.f ? a.c_pv / sum : 0.f;
@@ -346,38 +301,70 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
     const int8_t* vbase = PAGED ? nullptr : a.v + (size_t)row * a.batch + (size_t)head * dh;
     int8_t* stage = lds + wave * kWave;
     int key = kbegin + (WK == 1 ? 0 : kAttnKeys * wave);
-    if (PAGED && key < kend) at.look(key);
-    for (; key < kend; key += kAttnKeys * WK) {
-      v4i kf[4][KS], vf[NB];
-      bool there = true;
+    v4i kf[4][KS], vf[NB];
+    bool there = true;
+    auto load_keys = [&](int key) {
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const int8_t* kp;
+        if constexpr (PAGED)
+          kp = at.keys_of(key) + 4 * j * dh;
+        else
+          kp = kbase + (size_t)min(key + 16 * ((lane >> 2) & 3) + 4 * j + (lane & 3), kend - 1) * a.ld;
+#pragma unroll
+        for (int s = 0; s < KS; ++s) kf[j][s] = *(const v4i*)(kp + slice[s]);
+      }
+    };
+    v4i vr[PAGED ? 1 : 4][KS];  // an encoder's values: 4 keys (4 (l mod 16) ..) and 16 columns of each slice
+    auto load_values = [&](int key) {
       if constexpr (PAGED) {
-        const int8_t* kp = at.keys_of(key);
         const int8_t* vp = at.values_of(key);
         there = at.there();
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-          for (int s = 0; s < KS; ++s) kf[j][s] = *(const v4i*)(kp + 4 * j * dh + slice[s]);
-#pragma unroll
         for (int b = 0; b < NB; ++b) vf[b] = *(const v4i*)(vp + 256 * b);
-        at.look(min(key + kAttnKeys * WK, kend - 1));
       } else {
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const int8_t* kp = kbase + (size_t)min(key + 16 * ((lane >> 2) & 3) + 4 * j + (lane & 3), kend - 1) * a.ld;
-#pragma unroll
-          for (int s = 0; s < KS; ++s) kf[j][s] = *(const v4i*)(kp + slice[s]);
-        }
-        // values: a lane takes 4 keys (4 (l mod 16) ..) and 16 columns, and
-        // stores dwords of 4 keys; chunks of 16 keys are swapped about by
-        // column so that neither side meets bank conflicts
-        v4i vr[4][KS];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
           const int8_t* vp = vbase + (size_t)min(key + 4 * col + i, kend - 1) * a.ld;
 #pragma unroll
           for (int s = 0; s < KS; ++s) vr[i][s] = *(const v4i*)(vp + slice[s]);
         }
+      }
+    };
+    if (key < kend) {
+      if constexpr (PAGED) at.look(key);
+      load_keys(key);
+      load_values(key);
+      if constexpr (PAGED) at.look(min(key + kAttnKeys * WK, kend - 1));
+    }
+    for (; key < kend; key += kAttnKeys * WK) {
+      const bool more = key + kAttnKeys * WK < kend;
+      // scores less the reference: the lane's query, keys key + 16 g + 4 j + i
+      v4i d[4], p[3];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        d[j] = mfma16(kf[j][0], t.q[0], v4i{-y.ref, -y.ref, -y.ref, -y.ref});
+#pragma unroll
+        for (int s = 1; s < KS; ++s) d[j] = mfma16(kf[j][s], t.q[s], d[j]);
+      }
+      // the next step's keys take these registers while this step's weights are
+      // computed, its values the values' while the next scores are
+      if (more) load_keys(key + kAttnKeys * WK);
+      const bool masked = key + kAttnKeys > all_see || __any(!there);
+      const int count = there ? min(t.mine, kend) - key - 16 * g : 0;
+      const int up = max(quad_max(largest(d, masked, count)), 0);
+      const float scale = __builtin_amdgcn_exp2f(-(float)up * a.c2);
+#pragma unroll
+      for (int j = 0; j < 4; ++j)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) d[j][i] -= up;  // (masked places stay far below)
+      float x[4][4];
+      exponents(d, masked, count, a.c2, x);
+      y.sum = fmaf(y.sum, scale, digits(x, p));
+      y.ref += up;
+      if constexpr (!PAGED) {
+        // dwords of 4 keys go to LDS, chunks of 16 keys swapped about by column so
+        // that neither side meets bank conflicts
 #pragma unroll
         for (int s = 0; s < KS; ++s) {
           if (64 * s + 16 * g < dh) {
@@ -403,19 +390,17 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
         __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
         __builtin_amdgcn_wave_barrier();
       }
-      // scores less the reference: the lane's query, keys key + 16 g + 4 j + i
-      v4i d[4], p[3];
 #pragma unroll
-      for (int j = 0; j < 4; ++j) {
-        d[j] = mfma16(kf[j][0], t.q[0], v4i{-y.ref, -y.ref, -y.ref, -y.ref});
-#pragma unroll
-        for (int s = 1; s < KS; ++s) d[j] = mfma16(kf[j][s], t.q[s], d[j]);
+      for (int b = 0; b < NB; ++b) {
+        const v4i none{0, 0, 0, 0};
+        y.fold(b, scale, mfma16(vf[b], p[0], none), mfma16(vf[b], p[1], none), mfma16(vf[b], p[2], none));
       }
-      y.weigh(d, key + kAttnKeys > all_see || __any(!there), there ? min(t.mine, kend) - key - 16 * g : 0, a.c2, p);
-#pragma unroll
-      for (int b = 0; b < NB; ++b) y.add(b, vf[b], p);
+      if (more) {
+        load_values(key + kAttnKeys * WK);
+        if constexpr (PAGED) at.look(min(key + 2 * kAttnKeys * WK, kend - 1));
+      }
     }
-    y.close();
+    y.sum = quad_sum(y.sum);
     if constexpr (WK == 1) {
       if (live == 1)
         y.store(a, t, lane);
@@ -452,7 +437,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
         }
         if (live == 1) {
           store_joined(a, w, head, 16 * tile + q, c, dh, o, wsum);
-        } else {
+        } else if ((16 * tile + q) / a.group < w.n) {
           if (c == 0) {
             part[16 * dh + q] = wsum;
             part[16 * dh + 16 + q] = top;
@@ -549,7 +534,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_top(AttnArgs a) {
 #pragma unroll
           for (int s = 1; s < KS; ++s) d[j] = mfma16(kc[j][s], q[x][s], d[j]);
         }
-        top[x] = max(top[x], TileSums<NB>::largest(d, masked, here ? seen[x] - now - 16 * g : 0));
+        top[x] = max(top[x], largest(d, masked, here ? seen[x] - now - 16 * g : 0));
       }
     }
 #pragma unroll
@@ -699,7 +684,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
       fetch_values(kbegin, vbuf);
       look(kbegin + kAttnKeys);
       transpose(vbuf);
-      v4i p[QT][3];
+      v4i acc[QT][3][NB], p[QT][3];
       int8_t *v_prev = vbuf + 2 * kValueBytes, *v_cur = vbuf, *v_next = vbuf + kValueBytes;
       auto values = [&](v4i (&v)[NB]) {
 #pragma unroll
@@ -709,7 +694,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
 #pragma unroll
         for (int b = 0; b < NB; ++b)
 #pragma unroll
-          for (int x = 0; x < QT; ++x) y[x].add(b, v[b], p[x]);
+          for (int x = 0; x < QT; ++x)
+#pragma unroll
+            for (int i = 0; i < 3; ++i) acc[x][i][b] = mfma16(v[b], p[x][i], acc[x][i][b]);
       };
       int key = kbegin;
       do {
@@ -717,7 +704,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
 #pragma unroll
         for (int x = 0; x < QT; ++x)
 #pragma unroll
-          for (int i = 0; i < 3; ++i) p[x][i] = v4i{0, 0, 0, 0};
+          for (int i = 0; i < 3; ++i) {
+            p[x][i] = v4i{0, 0, 0, 0};
+#pragma unroll
+            for (int b = 0; b < NB; ++b) acc[x][i][b] = v4i{0, 0, 0, 0};
+          }
         for (; key < pend; key += kAttnKeys, cur ^= 1) {
           there = next_there;
           landed();
@@ -736,12 +727,12 @@ __global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
           const bool masked = key + kAttnKeys > all_see || __any(!there);
 #pragma unroll
           for (int i = 0; i < QT; ++i)
-            TileSums<NB>::exponents(d[i], masked, there ? min(t[i].mine, kend) - key - 16 * g : 0, a.c2, x[i]);
+            exponents(d[i], masked, there ? min(t[i].mine, kend) - key - 16 * g : 0, a.c2, x[i]);
           __builtin_amdgcn_sched_barrier(0);
           v4i p_new[QT][3];
           products(v);
 #pragma unroll
-          for (int i = 0; i < QT; ++i) y[i].digits(x[i], p_new[i]);
+          for (int i = 0; i < QT; ++i) y[i].sum += digits(x[i], p_new[i]);
           // one matrix instruction, then its share of the others
 #pragma unroll
           for (int i = 0; i < 3 * NB * QT; ++i) {
@@ -763,7 +754,9 @@ __global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
         values(v);
         products(v);
 #pragma unroll
-        for (int i = 0; i < QT; ++i) y[i].fold();
+        for (int i = 0; i < QT; ++i)
+#pragma unroll
+          for (int b = 0; b < NB; ++b) y[i].fold(b, 1.f, acc[i][0][b], acc[i][1][b], acc[i][2][b]);
       } while (LONG && key < kend);
     }
 #pragma unroll
@@ -796,7 +789,9 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
       if (m / a.group >= w.n) continue;
       float top = (float)kNoReference, sum = 0.f;
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 8
       for (int s = 0; s < live; ++s) top = fmaxf(top, part[(size_t)s * (16 * (dh + 2)) + 16 * dh + 16 + q]);
+#pragma unroll 8
       for (int s = 0; s < live; ++s) {
         const float* src = part + (size_t)s * (16 * (dh + 2));
         const float scale = __builtin_amdgcn_exp2f((src[16 * dh + 16 + q] - top) * a.c2);

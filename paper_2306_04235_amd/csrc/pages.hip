@@ -374,18 +374,24 @@ __global__ __launch_bounds__(256) void k_pages_write(PagesWrite w) {
     const int lo = max(begin - 16 * g, 0), hi = min(end - 16 * g, 16), g_in = g & ((w.s.page_size >> 4) - 1);
     const long t0 = 16L * g - off;  // token at the group's first place (before the first new one where lo > 0)
     const int cpr = D / 16;
-    for (int i = threadIdx.x; i < (hi - lo) * cpr; i += 256) {
+    auto key_to = [&](int i) {  // chunk i of the new keys' 16-byte chunks
       const int t = lo + i / cpr, c = 16 * (i % cpr), head = c / dh;
-      *(v4i*)(kp + ((size_t)head * w.s.page_size + 16 * g_in + t) * dh + c % dh) =
-          *(const v4i*)(w.k + (t0 + t) * w.ld + c);
-    }
+      return (v4i*)(kp + ((size_t)head * w.s.page_size + 16 * g_in + t) * dh + c % dh);
+    };
+    auto key_from = [&](int i) { return *(const v4i*)(w.k + (t0 + lo + i / cpr) * w.ld + 16 * (i % cpr)); };
     if (hi - lo == 16) {
-      for (int i = threadIdx.x; i < D / 4; i += 256) {
-        const int c = 4 * i, head = c / dh;
-        uint32_t x[16];
+      // D chunks of keys, four to a thread, beside D / 4 dword columns of
+      // values, one to a thread: all loads before the stores
+      for (int i0 = threadIdx.x; i0 < D / 4; i0 += 256) {
+        const int c = 4 * i0, head = c / dh;
+        v4i k[4];
+        uint32_t x[16], y[4][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) k[q] = key_from(i0 + q * (D / 4));
 #pragma unroll
         for (int t = 0; t < 16; ++t) x[t] = *(const uint32_t*)(w.v + (t0 + t) * w.ld + c);
-        uint32_t y[4][4];
+#pragma unroll
+        for (int q = 0; q < 4; ++q) *key_to(i0 + q * (D / 4)) = k[q];
 #pragma unroll
         for (int q = 0; q < 4; ++q) transpose4(x + 4 * q, y[0][q], y[1][q], y[2][q], y[3][q]);
         v4i* out = (v4i*)(vp + ((size_t)(head * (w.s.page_size >> 4) + g_in) * dh + c % dh) * 16);
@@ -393,6 +399,7 @@ __global__ __launch_bounds__(256) void k_pages_write(PagesWrite w) {
         for (int b = 0; b < 4; ++b) out[b] = v4i{(int)y[b][0], (int)y[b][1], (int)y[b][2], (int)y[b][3]};
       }
     } else {
+      for (int i = threadIdx.x; i < (hi - lo) * cpr; i += 256) *key_to(i) = key_from(i);
       for (int i = threadIdx.x; i < (hi - lo) * (D / 4); i += 256) {
         const int t = lo + i / (D / 4), c = 4 * (i % (D / 4)), head = c / dh;
         const uint32_t x = *(const uint32_t*)(w.v + (t0 + t) * w.ld + c);
