@@ -771,38 +771,65 @@ __global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
   }
 }
 
-// Joins the key ranges of a query tile; one block per tile.
+// Joins the key ranges of a query tile; one block per query: a thread takes four
+// columns of every kParts-th range, eight of them at once, and the threads of a
+// column then join theirs.  The ranges are read before it is known how many there
+// are (what lies behind the last is not used).
 template <int NB>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  constexpr int dh = 16 * NB;
+  constexpr int dh = 16 * NB, kPart = 16 * (dh + 2), U = 8;
+  constexpr int kCols = dh / 4, kParts = 256 / kCols < 16 ? 256 / kCols : 16;
+  __shared__ float4 ys[kParts][kCols];
+  __shared__ float tops[kParts], sums[kParts];
   const int per_row = a.n_kv_heads * a.tiles;
   const int row = blockIdx.x / per_row, head = blockIdx.x % per_row / a.tiles;
+  const int mine = threadIdx.x / kCols, col = threadIdx.x % kCols;
   const AttnRow w = attn_row(a, row);
   for (int tile = blockIdx.x % a.tiles; 16 * tile < w.n * a.group; tile += a.tiles) {
     // a chunk's ranges go by its block's last tile
     const int span = a.waves == 0 ? 4 * chunk_tiles(NB) : 1, last = (w.n * a.group + 15) / 16 - 1;
     const int live = live_splits(a, tile_keys(a, w, min(tile / span * span + span - 1, last)));
     if (live == 1) continue;
-    const float* part = a.part + tile_slot(a, w, row, head, tile, 0) * (16 * (dh + 2));
-    for (int i = threadIdx.x; i < 16 * dh / 4; i += 256) {
-      const int q = i / (dh / 4), c = 4 * (i % (dh / 4)), m = 16 * tile + q;
-      if (m / a.group >= w.n) continue;
+    const float* part = a.part + tile_slot(a, w, row, head, tile, 0) * kPart;
+    for (int q = blockIdx.y; q < min(16, w.n * a.group - 16 * tile); q += gridDim.y) {
       float top = (float)kNoReference, sum = 0.f;
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 8
-      for (int s = 0; s < live; ++s) top = fmaxf(top, part[(size_t)s * (16 * (dh + 2)) + 16 * dh + 16 + q]);
-#pragma unroll 8
-      for (int s = 0; s < live; ++s) {
-        const float* src = part + (size_t)s * (16 * (dh + 2));
-        const float scale = __builtin_amdgcn_exp2f((src[16 * dh + 16 + q] - top) * a.c2);
-        const float4 x = *(const float4*)(src + q * dh + c);
-        sum = fmaf(scale, src[16 * dh + q], sum);
-        y.x = fmaf(scale, x.x, y.x);
-        y.y = fmaf(scale, x.y, y.y);
-        y.z = fmaf(scale, x.z, y.z);
-        y.w = fmaf(scale, x.w, y.w);
+      auto join = [&](float ref, float s, float4 x) {
+        const float best = fmaxf(top, ref);
+        const float old = __builtin_amdgcn_exp2f((top - best) * a.c2), now = __builtin_amdgcn_exp2f((ref - best) * a.c2);
+        top = best;
+        sum = fmaf(sum, old, s * now);
+        y = make_float4(fmaf(y.x, old, x.x * now), fmaf(y.y, old, x.y * now), fmaf(y.z, old, x.z * now),
+                        fmaf(y.w, old, x.w * now));
+      };
+      if (mine < kParts) {
+        for (int s0 = mine; s0 < live; s0 += U * kParts) {
+          float s[U], ref[U];
+          float4 x[U];
+#pragma unroll
+          for (int u = 0; u < U; ++u) {
+            const float* src = part + (size_t)min(s0 + u * kParts, a.splits - 1) * kPart;
+            s[u] = src[16 * dh + q];
+            ref[u] = src[16 * dh + 16 + q];
+            x[u] = *(const float4*)(src + q * dh + 4 * col);
+          }
+#pragma unroll
+          for (int u = 0; u < U; ++u)
+            if (s0 + u * kParts < live) join(ref[u], s[u], x[u]);
+        }
+        ys[mine][col] = y;
+        if (col == 0) {
+          tops[mine] = top;
+          sums[mine] = sum;
+        }
       }
-      store_joined(a, w, head, m, c, dh, y, sum);
+      __syncthreads();
+      if (mine == 0) {
+#pragma unroll
+        for (int p = 1; p < kParts; ++p) join(tops[p], sums[p], ys[p][col]);
+        store_joined(a, w, head, 16 * tile + q, 4 * col, dh, y, sum);
+      }
+      __syncthreads();
     }
   }
 }
@@ -822,7 +849,8 @@ hipError_t launch_attn_nb(const AttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((k_attn<NB, PAGED, 1>), dim3((units + 3) / 4), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((k_attn<NB, PAGED, 4>), dim3(units), dim3(256), 0, s, a);
-  if (a.splits > 1) hipLaunchKernelGGL((k_attn_join<NB>), dim3(tiles), dim3(256), 0, s, a);
+  if (a.splits > 1)
+    hipLaunchKernelGGL((k_attn_join<NB>), dim3(tiles, a.queries), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

@@ -79,6 +79,7 @@ int run_attn(AttnArgs& a, bool paged, int d_head, int max_q, int max_len, void* 
   a.splits = p.splits;
   a.chunk = p.chunk;
   a.waves = p.waves;
+  a.queries = p.queries;
   a.part = static_cast<float*>(d_ws);
   a.tops = reinterpret_cast<int*>(static_cast<char*>(d_ws) + p.part_bytes);
   const hipError_t h = launch_attn(a, paged, d_head, static_cast<hipStream_t>(stream));
@@ -93,14 +94,21 @@ AttnPlan plan_attn(int rows, int n, int n_kv_heads, int group, int d_head, int m
   const long tiles = std::max(1L, ((long)max_q * group + 15) / 16);
   p.tiles = (int)std::min(tiles, kMaxAttnUnits / std::max(1L, heads));  // (a block goes on to further tiles)
   const long units = heads * p.tiles;
+  p.queries = (int)std::max(1L, std::min(16L, (long)max_q * group));
   p.splits = 1;
   p.chunk = 1 << 30;
   p.waves = max_len <= 128 || units >= 2048 ? 1 : 4;
   if (p.tiles >= 4 && max_len > 64) {
     p.waves = 0;
     p.tiles = (p.tiles + 7) / 8 * 8;
-  } else if (p.waves == 4 && max_len > 256 && units < 1024) {
-    const long want = std::min((1024 + units - 1) / units, (long)(max_len + 255) / 256);
+    const long blocks = heads * p.tiles / (d_head <= 64 ? 8 : 4);
+    const long want = std::min((512 + blocks - 1) / blocks, (long)(max_len + 1023) / 1024);
+    if (want > 1) {
+      p.chunk = (int)((max_len + want - 1) / want + 255) / 256 * 256;
+      p.splits = (max_len + p.chunk - 1) / p.chunk;
+    }
+  } else if (p.waves == 4 && max_len > 512 && units < 2048) {
+    const long want = std::min((2048 + units - 1) / units, (long)(max_len + 511) / 512);
     if (want > 1) {
       p.chunk = (int)((max_len + want - 1) / want + 255) / 256 * 256;
       p.splits = (max_len + p.chunk - 1) / p.chunk;

@@ -49,7 +49,7 @@ struct AttnArgs {
   float c2, c_pv;  // c_qk log2 e; values' scale
   // the launch (AttnPlan): query tiles per row and key head in the grid, key
   // ranges of `chunk` keys per tile, their partial results, a chunk's maxima
-  int tiles, splits, chunk, waves;
+  int tiles, splits, chunk, waves, queries;
   float* part;
   int* tops;
   // keys and values: pages of one layer, or rows [sentence][S]
@@ -65,7 +65,8 @@ struct AttnArgs {
 // The launch of a call, by the caller's bounds, and the workspace that it needs.
 struct AttnPlan {
   int tiles, splits, chunk;
-  int waves;  // per query tile: 1 or 4; 0: the chunk kernels
+  int waves;    // per query tile: 1 or 4; 0: the chunk kernels
+  int queries;  // of a tile
   size_t part_bytes, ws_bytes;
 };
 AttnPlan plan_attn(int rows, int n, int n_kv_heads, int group, int d_head, int max_q, int max_len);
