@@ -24,6 +24,7 @@
 #pragma once
 
 #include <climits>
+#include <type_traits>
 
 #include "blocks.hpp"
 #include "cache.hpp"
@@ -183,21 +184,21 @@ __device__ __forceinline__ int largest(v4i (&d)[4], bool masked, int count) {
   return top;
 }
 
-// Exponents c2 d; -inf where masked.
-__device__ __forceinline__ void exponents(const v4i (&d)[4], bool masked, int count, float c2, float (&x)[4][4]) {
+// Exponents c2 d, and -inf in the place of those of masked keys.
+__device__ __forceinline__ void exponents(const v4i (&d)[4], float c2, float (&x)[4][4]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
     for (int i = 0; i < 4; ++i) x[j][i] = (float)d[j][i] * c2;
-  if (masked) {
+}
+__device__ __forceinline__ void hide(int count, float (&x)[4][4]) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
+  for (int j = 0; j < 4; ++j)
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        x[j][i] = 4 * j + i >= count ? -__builtin_inff() : x[j][i];
-        asm volatile("" : "+v"(x[j][i]));
-      }
-  }
+    for (int i = 0; i < 4; ++i) {
+      x[j][i] = 4 * j + i >= count ? -__builtin_inff() : x[j][i];
+      asm volatile("" : "+v"(x[j][i]));  // (as above)
+    }
 }
 
 // Digits of the weights 2^x; returns the weights' sum.
@@ -359,7 +360,8 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) d[j][i] -= up;  // (masked places stay far below)
       float x[4][4];
-      exponents(d, masked, count, a.c2, x);
+      exponents(d, a.c2, x);
+      if (masked) hide(count, x);
       y.sum = fmaf(y.sum, scale, digits(x, p));
       y.ref += up;
       if constexpr (!PAGED) {
@@ -525,17 +527,23 @@ __global__ __launch_bounds__(256, 2) void k_attn_top(AttnArgs a) {
         load(key);
         look(key + kStride);
       }
+      auto tiles_of = [&](auto hidden) {
 #pragma unroll
-      for (int x = 0; x < kTopTiles; ++x) {
-        v4i d[4];
+        for (int x = 0; x < kTopTiles; ++x) {
+          v4i d[4];
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          d[j] = mfma16(kc[j][0], q[x][0], v4i{0, 0, 0, 0});
+          for (int j = 0; j < 4; ++j) {
+            d[j] = mfma16(kc[j][0], q[x][0], v4i{0, 0, 0, 0});
 #pragma unroll
-          for (int s = 1; s < KS; ++s) d[j] = mfma16(kc[j][s], q[x][s], d[j]);
+            for (int s = 1; s < KS; ++s) d[j] = mfma16(kc[j][s], q[x][s], d[j]);
+          }
+          top[x] = max(top[x], largest(d, hidden, here ? seen[x] - now - 16 * g : 0));
         }
-        top[x] = max(top[x], largest(d, masked, here ? seen[x] - now - 16 * g : 0));
-      }
+      };
+      if (masked)
+        tiles_of(std::true_type{});
+      else
+        tiles_of(std::false_type{});
     }
 #pragma unroll
     for (int x = 0; x < kTopTiles; ++x) {
@@ -726,8 +734,11 @@ __global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
           }
           const bool masked = key + kAttnKeys > all_see || __any(!there);
 #pragma unroll
-          for (int i = 0; i < QT; ++i)
-            exponents(d[i], masked, there ? min(t[i].mine, kend) - key - 16 * g : 0, a.c2, x[i]);
+          for (int i = 0; i < QT; ++i) exponents(d[i], a.c2, x[i]);
+          if (masked) {
+#pragma unroll
+            for (int i = 0; i < QT; ++i) hide(there ? min(t[i].mine, kend) - key - 16 * g : 0, x[i]);
+          }
           __builtin_amdgcn_sched_barrier(0);
           v4i p_new[QT][3];
           products(v);

@@ -98,7 +98,7 @@ AttnPlan plan_attn(int rows, int n, int n_kv_heads, int group, int d_head, int m
   p.splits = 1;
   p.chunk = 1 << 30;
   p.waves = max_len <= 128 || units >= 2048 ? 1 : 4;
-  if (p.tiles >= 4 && max_len > 64) {
+  if (p.tiles >= 16 && max_len >= 512 && units >= 512) {
     p.waves = 0;
     p.tiles = (p.tiles + 7) / 8 * 8;
     const long blocks = heads * p.tiles / (d_head <= 64 ? 8 : 4);
