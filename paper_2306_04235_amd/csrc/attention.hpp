@@ -452,14 +452,16 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
   }
 }
 
-// The largest score of each query of a few tiles over a range of keys: the waves
+// The largest score of each query of eight tiles over a range of keys: the waves
 // take turns at the keys, straight from memory, one step ahead in registers, each
-// step against all of the block's queries.
-constexpr int top_tiles(int nb) { return nb <= 4 ? 8 : 4; }  // (their queries stay in registers)
+// step against all of the block's queries.  Bound by what the L2s deliver: blocks
+// of 2, 4 and 8 tiles take 172, 99 and 73 us (1699 queries of 16 heads over 6853
+// keys, heads of 128, and three shorter rows).
+constexpr int kTopTiles = 8;  // (their queries stay in registers)
 
 template <int NB, bool PAGED>
 __global__ __launch_bounds__(256, 2) void k_attn_top(AttnArgs a) {
-  constexpr int dh = 16 * NB, KS = (NB + 3) / 4, kStride = 4 * kAttnKeys, kTopTiles = top_tiles(NB);
+  constexpr int dh = 16 * NB, KS = (NB + 3) / 4, kStride = 4 * kAttnKeys;
   __shared__ int tops[4 * kTopTiles * 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
   const int groups = a.tiles / kTopTiles, per_head = groups * a.splits, per_row = per_head * a.n_kv_heads;
@@ -561,17 +563,20 @@ __global__ __launch_bounds__(256, 2) void k_attn_top(AttnArgs a) {
   }
 }
 
-// The query tiles of four waves, over the same keys: 64 of them at a time pass
+// The query tiles of a block's waves, over the same keys: 64 of them at a time pass
 // through LDS, in the order of the matrix operands (a kilobyte per operand, lane
 // by lane), so that a block reads them once.  A wave has two tiles where its
 // registers hold their sums at two waves per SIMD (heads of up to 64), and reads
-// each operand for both.  Keys, and the values of pages, come in by loads
-// straight to LDS, one step ahead; an encoder's values are transposed on the way,
-// each wave those of its 16 keys.
+// each operand for both.  Keys, and the values of pages, come in by loads straight
+// to LDS, one step ahead; an encoder's values are transposed on the way, each wave
+// those of its 16 keys.  (Eight waves to a block of wide heads read half as much
+// and are slower, 293 against 260 us in the case above: more of them wait for the
+// slowest.)
 //
 // The references are the scores' maxima, from k_attn_top: they never move, so that
 // the sums are integers throughout and no step branches.
 constexpr int chunk_tiles(int nb) { return nb <= 4 ? 2 : 1; }  // of a wave
+constexpr int kChunkWaves = 4;
 constexpr int kValueGap = 16;  // between values' operands: the transposing stores meet no bank conflicts
 
 __device__ __forceinline__ void load_to_lds(const int8_t* from, int8_t* to) {  // 16 bytes per lane, to + 16 lane
@@ -588,8 +593,8 @@ __device__ __forceinline__ void landed() {
 // LONG: ranges may hold more keys than the int32 sums (kFoldSteps); without it no
 // register holds sums in fp32 meanwhile.
 template <int NB, bool PAGED, bool LONG>
-__global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
-  constexpr int dh = 16 * NB, KS = (NB + 3) / 4, QT = chunk_tiles(NB), kTiles = 4 * QT;
+__global__ __launch_bounds__(64 * kChunkWaves, 2) void k_attn_chunk(AttnArgs a) {
+  constexpr int dh = 16 * NB, KS = (NB + 3) / 4, QT = chunk_tiles(NB), W = kChunkWaves, kTiles = W * QT;
   constexpr int kKeyBytes = 4 * KS * 1024, kValueBytes = NB * (1024 + kValueGap);
   __shared__ __attribute__((aligned(16))) int8_t kbuf[2 * kKeyBytes], vbuf[3 * kValueBytes];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -621,6 +626,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
     const int8_t* kbase = PAGED ? nullptr : a.k + (size_t)row * a.batch + (size_t)head * dh;
     const int8_t* vbase = PAGED ? nullptr : a.v + (size_t)row * a.batch + (size_t)head * dh;
     const int dc = lane >> 2, kg = lane & 3;  // transposing: 16 columns, 4 keys of the wave's 16
+    const bool transposes = dc < NB;
     v4i vr[4];
     bool there = true, next_there = true;
     auto fetch_keys = [&](int key, int8_t* buf) {  // operand (j, s) of keys 16 (l / 4 mod 4) + 4 j + l mod 4
@@ -638,17 +644,17 @@ __global__ __launch_bounds__(256, 2) void k_attn_chunk(AttnArgs a) {
       if constexpr (PAGED) {
         const int8_t* vp = at.values_of(key);
 #pragma unroll
-        for (int b = 0; b < NB; b += 4)
+        for (int b = 0; b < NB; b += W)
           if (b + wave < NB) load_to_lds(vp + 256 * (b + wave), buf + (b + wave) * (1024 + kValueGap));
-      } else {
+      } else if (transposes) {
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (dc < NB) vr[i] = *(const v4i*)(vbase + (size_t)min(key + 16 * wave + 4 * kg + i, kend - 1) * a.ld + 16 * dc);
+          vr[i] = *(const v4i*)(vbase + (size_t)min(key + 16 * wave + 4 * kg + i, kend - 1) * a.ld + 16 * dc);
       }
     };
     auto transpose = [&](int8_t* buf) {  // the values that fetch_values left in registers
       if constexpr (!PAGED) {
-        if (dc < NB) {
+        if (transposes) {
           uint32_t* to = (uint32_t*)(buf + dc * (1024 + kValueGap) + 256 * wave) + kg;
 #pragma unroll
           for (int c = 0; c < 4; ++c) {
@@ -798,7 +804,7 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   const AttnRow w = attn_row(a, row);
   for (int tile = blockIdx.x % a.tiles; 16 * tile < w.n * a.group; tile += a.tiles) {
     // a chunk's ranges go by its block's last tile
-    const int span = a.waves == 0 ? 4 * chunk_tiles(NB) : 1, last = (w.n * a.group + 15) / 16 - 1;
+    const int span = a.waves == 0 ? kChunkWaves * chunk_tiles(NB) : 1, last = (w.n * a.group + 15) / 16 - 1;
     const int live = live_splits(a, tile_keys(a, w, min(tile / span * span + span - 1, last)));
     if (live == 1) continue;
     const float* part = a.part + tile_slot(a, w, row, head, tile, 0) * kPart;
@@ -849,13 +855,13 @@ template <int NB, bool PAGED>
 hipError_t launch_attn_nb(const AttnArgs& a, hipStream_t s) {
   const int tiles = a.rows * a.n_kv_heads * a.tiles, units = tiles * a.splits;
   if (a.waves == 0)
-    hipLaunchKernelGGL((k_attn_top<NB, PAGED>), dim3(a.rows * a.n_kv_heads * (a.tiles / top_tiles(NB)) * a.splits),
+    hipLaunchKernelGGL((k_attn_top<NB, PAGED>), dim3(a.rows * a.n_kv_heads * (a.tiles / kTopTiles) * a.splits),
                        dim3(256), 0, s, a);
-  const dim3 chunks(a.rows * a.n_kv_heads * (a.tiles / (4 * chunk_tiles(NB))) * a.splits);
+  const dim3 chunks(a.rows * a.n_kv_heads * (a.tiles / (kChunkWaves * chunk_tiles(NB))) * a.splits);
   if (a.waves == 0 && a.cap <= kAttnKeys * kFoldSteps)
-    hipLaunchKernelGGL((k_attn_chunk<NB, PAGED, false>), chunks, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_attn_chunk<NB, PAGED, false>), chunks, dim3(64 * kChunkWaves), 0, s, a);
   else if (a.waves == 0)
-    hipLaunchKernelGGL((k_attn_chunk<NB, PAGED, true>), chunks, dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_attn_chunk<NB, PAGED, true>), chunks, dim3(64 * kChunkWaves), 0, s, a);
   else if (a.waves == 1)
     hipLaunchKernelGGL((k_attn<NB, PAGED, 1>), dim3((units + 3) / 4), dim3(256), 0, s, a);
   else
