@@ -98,6 +98,7 @@ struct PagedKeys {
   const int32_t* table;
   size_t koff, voff;
   int last, gk, gv, page_k, page_v;
+  // `keys`: where the look-ups end
   __device__ __forceinline__ PagedKeys(const AttnArgs& args, int row, int head, int lane, int keys) : a(args) {
     constexpr int dh = 16 * NB;
     table = a.table + (size_t)row * a.max_pages;
@@ -269,9 +270,10 @@ struct TileSums {
 
 // One query tile per wave (WK 1) or per block, whose four waves take turns at
 // the keys (WK 4).  For few queries per row: every wave loads its keys and
-// values straight into the matrix operands.
-template <int NB, bool PAGED, int WK>
-__global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
+// values straight into the matrix operands.  SHORT: rows of one or two steps, where
+// more waves at once are worth more than keys a step ahead.
+template <int NB, bool PAGED, int WK, bool SHORT>
+__global__ __launch_bounds__(256, !SHORT ? 2 : NB <= 4 ? 4 : 3) void k_attn(AttnArgs a) {
   constexpr int dh = 16 * NB, KS = (NB + 3) / 4;  // 64-wide slices of the head
   constexpr int kStage = PAGED ? 0 : NB * 1024;   // a wave's values, transposed
   constexpr int kJoin = WK == 1 ? 0 : 16 * (dh + 4) * 4 + 128;
@@ -297,7 +299,9 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
     int slice[KS];
 #pragma unroll
     for (int s = 0; s < KS; ++s) slice[s] = 64 * s + 16 * g < dh ? 64 * s + 16 * g : 0;
-    PagedKeys<NB> at(a, PAGED ? row : 0, head, lane, kend);
+    // (a short row's look-ups do not wait for its length: what lies behind it may be
+    // any number, and is hidden)
+    PagedKeys<NB> at(a, PAGED ? row : 0, head, lane, SHORT ? a.cap : kend);
     const int8_t* kbase = PAGED ? nullptr : a.k + (size_t)row * a.batch + (size_t)head * dh;
     const int8_t* vbase = PAGED ? nullptr : a.v + (size_t)row * a.batch + (size_t)head * dh;
     int8_t* stage = lds + wave * kWave;
@@ -332,14 +336,19 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
         }
       }
     };
-    if (key < kend) {
-      if constexpr (PAGED) at.look(key);
+    if (PAGED && (SHORT || key < kend)) at.look(key);
+    if (!SHORT && key < kend) {
       load_keys(key);
       load_values(key);
       if constexpr (PAGED) at.look(min(key + kAttnKeys * WK, kend - 1));
     }
     for (; key < kend; key += kAttnKeys * WK) {
       const bool more = key + kAttnKeys * WK < kend;
+      if (SHORT) {
+        load_keys(key);
+        load_values(key);
+        if (PAGED && more) at.look(key + kAttnKeys * WK);
+      }
       // scores less the reference: the lane's query, keys key + 16 g + 4 j + i
       v4i d[4], p[3];
 #pragma unroll
@@ -350,7 +359,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
       }
       // the next step's keys take these registers while this step's weights are
       // computed, its values the values' while the next scores are
-      if (more) load_keys(key + kAttnKeys * WK);
+      if (!SHORT && more) load_keys(key + kAttnKeys * WK);
       const bool masked = key + kAttnKeys > all_see || __any(!there);
       const int count = there ? min(t.mine, kend) - key - 16 * g : 0;
       const int up = max(quad_max(largest(d, masked, count)), 0);
@@ -397,7 +406,7 @@ __global__ __launch_bounds__(256, 2) void k_attn(AttnArgs a) {
         const v4i none{0, 0, 0, 0};
         y.fold(b, scale, mfma16(vf[b], p[0], none), mfma16(vf[b], p[1], none), mfma16(vf[b], p[2], none));
       }
-      if (more) {
+      if (!SHORT && more) {
         load_values(key + kAttnKeys * WK);
         if constexpr (PAGED) at.look(min(key + 2 * kAttnKeys * WK, kend - 1));
       }
@@ -862,10 +871,12 @@ hipError_t launch_attn_nb(const AttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((k_attn_chunk<NB, PAGED, false>), chunks, dim3(64 * kChunkWaves), 0, s, a);
   else if (a.waves == 0)
     hipLaunchKernelGGL((k_attn_chunk<NB, PAGED, true>), chunks, dim3(64 * kChunkWaves), 0, s, a);
+  else if (a.waves == 1 && a.is_short)
+    hipLaunchKernelGGL((k_attn<NB, PAGED, 1, true>), dim3((units + 3) / 4), dim3(256), 0, s, a);
   else if (a.waves == 1)
-    hipLaunchKernelGGL((k_attn<NB, PAGED, 1>), dim3((units + 3) / 4), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_attn<NB, PAGED, 1, false>), dim3((units + 3) / 4), dim3(256), 0, s, a);
   else
-    hipLaunchKernelGGL((k_attn<NB, PAGED, 4>), dim3(units), dim3(256), 0, s, a);
+    hipLaunchKernelGGL((k_attn<NB, PAGED, 4, false>), dim3(units), dim3(256), 0, s, a);
   if (a.splits > 1)
     hipLaunchKernelGGL((k_attn_join<NB>), dim3(tiles, a.queries), dim3(256), 0, s, a);
   return hipGetLastError();

@@ -80,6 +80,7 @@ int run_attn(AttnArgs& a, bool paged, int d_head, int max_q, int max_len, void* 
   a.chunk = p.chunk;
   a.waves = p.waves;
   a.queries = p.queries;
+  a.is_short = p.is_short;
   a.part = static_cast<float*>(d_ws);
   a.tops = reinterpret_cast<int*>(static_cast<char*>(d_ws) + p.part_bytes);
   const hipError_t h = launch_attn(a, paged, d_head, static_cast<hipStream_t>(stream));
@@ -97,7 +98,8 @@ AttnPlan plan_attn(int rows, int n, int n_kv_heads, int group, int d_head, int m
   p.queries = (int)std::max(1L, std::min(16L, (long)max_q * group));
   p.splits = 1;
   p.chunk = 1 << 30;
-  p.waves = max_len <= 128 || units >= 2048 ? 1 : 4;
+  p.is_short = max_len <= 128;
+  p.waves = p.is_short || units >= 2048 ? 1 : 4;
   if (p.tiles >= 16 && max_len >= 512 && units >= 512) {
     p.waves = 0;
     p.tiles = (p.tiles + 7) / 8 * 8;

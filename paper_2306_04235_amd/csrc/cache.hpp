@@ -50,6 +50,7 @@ struct AttnArgs {
   // the launch (AttnPlan): query tiles per row and key head in the grid, key
   // ranges of `chunk` keys per tile, their partial results, a chunk's maxima
   int tiles, splits, chunk, waves, queries;
+  bool is_short;
   float* part;
   int* tops;
   // keys and values: pages of one layer, or rows [sentence][S]
@@ -67,6 +68,7 @@ struct AttnPlan {
   int tiles, splits, chunk;
   int waves;    // per query tile: 1 or 4; 0: the chunk kernels
   int queries;  // of a tile
+  bool is_short;
   size_t part_bytes, ws_bytes;
 };
 AttnPlan plan_attn(int rows, int n, int n_kv_heads, int group, int d_head, int max_q, int max_len);
