@@ -350,6 +350,7 @@ __global__ __launch_bounds__(256) void k_compact_apply(PagesFork f, const int* t
 // transposes dwords of 16 tokens in registers and stores 64 bytes per thread;
 // one that has part of it stores bytes.
 __global__ __launch_bounds__(256) void k_pages_write(PagesWrite w) {
+  __shared__ v4i turn[4][256];
   const int r = blockIdx.x;
   int a, n;
   if (w.start) {
@@ -381,22 +382,38 @@ __global__ __launch_bounds__(256) void k_pages_write(PagesWrite w) {
     auto key_from = [&](int i) { return *(const v4i*)(w.k + (t0 + lo + i / cpr) * w.ld + 16 * (i % cpr)); };
     if (hi - lo == 16) {
       // D chunks of keys, four to a thread, beside D / 4 dword columns of
-      // values, one to a thread: all loads before the stores
-      for (int i0 = threadIdx.x; i0 < D / 4; i0 += 256) {
-        const int c = 4 * i0, head = c / dh;
+      // values, one to a thread: all loads before the stores.  A thread's four
+      // columns pass through LDS, so that a wave stores whole kilobytes.
+      for (int base = 0; base < D / 4; base += 256) {
+        const int i0 = base + threadIdx.x, lane = threadIdx.x & 63, from = base + (threadIdx.x & ~63);
+        const bool mine = i0 < D / 4;
         v4i k[4];
         uint32_t x[16], y[4][4];
+        if (mine) {
 #pragma unroll
-        for (int q = 0; q < 4; ++q) k[q] = key_from(i0 + q * (D / 4));
+          for (int q = 0; q < 4; ++q) k[q] = key_from(i0 + q * (D / 4));
 #pragma unroll
-        for (int t = 0; t < 16; ++t) x[t] = *(const uint32_t*)(w.v + (t0 + t) * w.ld + c);
+          for (int t = 0; t < 16; ++t) x[t] = *(const uint32_t*)(w.v + (t0 + t) * w.ld + 4 * i0);
 #pragma unroll
-        for (int q = 0; q < 4; ++q) *key_to(i0 + q * (D / 4)) = k[q];
+          for (int q = 0; q < 4; ++q) *key_to(i0 + q * (D / 4)) = k[q];
 #pragma unroll
-        for (int q = 0; q < 4; ++q) transpose4(x + 4 * q, y[0][q], y[1][q], y[2][q], y[3][q]);
-        v4i* out = (v4i*)(vp + ((size_t)(head * (w.s.page_size >> 4) + g_in) * dh + c % dh) * 16);
+          for (int q = 0; q < 4; ++q) transpose4(x + 4 * q, y[0][q], y[1][q], y[2][q], y[3][q]);
 #pragma unroll
-        for (int b = 0; b < 4; ++b) out[b] = v4i{(int)y[b][0], (int)y[b][1], (int)y[b][2], (int)y[b][3]};
+          for (int b = 0; b < 4; ++b)  // (places swapped about by lane: no bank conflicts)
+            turn[threadIdx.x >> 6][4 * lane + (b ^ (lane >> 1 & 3))] = v4i{(int)y[b][0], (int)y[b][1], (int)y[b][2], (int)y[b][3]};
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
+        __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+#pragma unroll
+        for (int q = 0; q < 4; ++q) {
+          const int c = 64 * q + lane, col = 4 * from + c, head = col / dh, at = c >> 2;
+          if (col < D)
+            *(v4i*)(vp + ((size_t)(head * (w.s.page_size >> 4) + g_in) * dh + col % dh) * 16) =
+                turn[threadIdx.x >> 6][4 * at + ((c & 3) ^ (at >> 1 & 3))];
+        }
+        __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+        __builtin_amdgcn_wave_barrier();
       }
     } else {
       for (int i = threadIdx.x; i < (hi - lo) * cpr; i += 256) *key_to(i) = key_from(i);
