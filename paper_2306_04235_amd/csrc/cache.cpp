@@ -72,6 +72,7 @@ const char* attn_of(const mnmt_attn_cfg* c, int n_kv_heads, int d_head, AttnArgs
 }
 
 int run_attn(AttnArgs& a, bool paged, int d_head, int max_q, int max_len, void* d_ws, size_t ws_bytes, void* stream) {
+  if ((long)a.n * a.group > (1L << 30)) return bad("n * n_heads / n_kv_heads must be at most 2^30");
   const AttnPlan p = plan_attn(a.rows, a.n, a.n_kv_heads, a.group, d_head, std::min(max_q, a.n), max_len);
   if (p.ws_bytes > ws_bytes) return bad("the workspace is smaller than mnmt_attn_ws_bytes");
   if (p.ws_bytes && (!d_ws || !aligned(d_ws, 16))) return bad("the workspace must be 16-byte aligned and not null");
@@ -223,7 +224,8 @@ extern "C" int mnmt_pages_write(const mnmt_pages_cfg* cfg, void* d_pool, int lay
 extern "C" size_t mnmt_attn_ws_bytes(int rows, int n, int n_heads, int n_kv_heads, int d_head, int max_q,
                                      int max_len) {
   if (rows < 1 || n < 1 || n_kv_heads < 1 || (long)rows * n_kv_heads > kMaxAttnUnits || n_kv_heads > 256 || n_heads < 1 || n_heads > 4096 ||
-      n_heads % n_kv_heads || d_head < 16 || d_head > 128 || d_head % 16 || max_q < 0 || max_len < 0)
+      n_heads % n_kv_heads || (long)n * (n_heads / n_kv_heads) > (1L << 30) || d_head < 16 || d_head > 128 ||
+      d_head % 16 || max_q < 0 || max_len < 0)
     return 0;
   return plan_attn(rows, n, n_kv_heads, n_heads / n_kv_heads, d_head, std::min(max_q, n), max_len).ws_bytes;
 }

@@ -348,13 +348,6 @@ def _codes(name, t, width, device):
     return stride if n > 1 else w
 
 
-def _device(t):
-    """The device of a call; on it the launches and the current stream have to be."""
-    device = t.get_device()
-    _need(device >= 0, f"the tensors must be on a GPU, not on {t.device}")
-    return device
-
-
 def _workspace(nbytes, like, stream):
     """A call's own workspace, so that calls on different streams and captured graphs never share one."""
     t = _torch.empty(nbytes, dtype=_torch.uint8, device=like.device)
@@ -363,33 +356,32 @@ def _workspace(nbytes, like, stream):
     return t
 
 
-def _on_device(f):
-    """Imports torch on the first call, and makes the device of the first tensor the current one for the call."""
-
-    @functools.wraps(f)
-    def call(first, *args, **kw):
-        global _torch, _int8, _int32
-        if _torch is None:
-            import torch
-
-            _int8, _int32, _torch = torch.int8, torch.int32, torch
-        device = first.get_device()
-        if device < 0 or device == _torch.cuda.current_device():
-            return f(first, *args, **kw)
-        with _torch.cuda.device(device):
-            return f(first, *args, **kw)
-
-    return call
+_torch = _int8 = _int32 = _current = None
 
 
-_torch = _int8 = _int32 = None
+def _with_torch():
+    """torch, imported on the first call that gets tensors, and what every call takes from it."""
+    global _torch, _int8, _int32, _current
+    import torch
+
+    _int8, _int32 = torch.int8, torch.int32
+    _current = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+    _torch = torch
 
 
-@_on_device
+def _elsewhere(device, call, *args):
+    """The call with the tensors' device as the current one: its launches and its stream belong there."""
+    _need(device >= 0, "the tensors must be on a GPU")
+    with _torch.cuda.device(device):
+        return call(*args)
+
+
 def mnmt_pages_fork(pool, table, lens, parent=None, new=None, out=None, stream=None):
     """The next step's tables: row r goes on from row parent[r] (outside the table: empty; None: itself) with room for
     new[r] more tokens.  Returns (table int32 [rows, max_pages], lengths int32 [rows], info int32 [2]: free pages left,
     pages missing); out: these three tensors."""
+    if _torch is None:
+        _with_torch()
     rows_in, width = table.shape
     rows = rows_in if parent is None else parent.shape[0]
     _, cfg, nbytes = _pool(pool, width, rows)
@@ -400,7 +392,8 @@ def mnmt_pages_fork(pool, table, lens, parent=None, new=None, out=None, stream=N
         _ints("parent", parent, (rows,), at)
     if new is not None:
         _ints("new", new, (rows,), at)
-    _device(pool)
+    if at < 0 or at != _current():
+        return _elsewhere(at, mnmt_pages_fork, pool, table, lens, parent, new, out, stream)
     if out is None:
         # one allocation: the lengths and the counts lie behind the table
         flat = _torch.empty(rows * (width + 1) + 2, dtype=_int32, device=pool.device)
@@ -417,16 +410,18 @@ def mnmt_pages_fork(pool, table, lens, parent=None, new=None, out=None, stream=N
     return out
 
 
-@_on_device
 def mnmt_pages_compact(pool, table, lens, out=None, stream=None):
     """Moves the pages in use to the lowest numbers.  Returns (table int32 [rows, max_pages], info int32 [2]: live pages,
     pages moved); out: these two tensors (out[0] may be the table itself)."""
+    if _torch is None:
+        _with_torch()
     rows, width = table.shape
     _, cfg, nbytes = _pool(pool, width, rows)
     at = pool.get_device()
     _ints("table", table, (rows, width), at)
     _ints("lens", lens, (rows,), at)
-    _device(pool)
+    if at < 0 or at != _current():
+        return _elsewhere(at, mnmt_pages_compact, pool, table, lens, out, stream)
     if out is None:
         flat = _torch.empty(rows * width + 2, dtype=_int32, device=pool.device)
         out = (flat[:-2].view(rows, width), flat[-2:])
@@ -441,10 +436,11 @@ def mnmt_pages_compact(pool, table, lens, out=None, stream=None):
     return out
 
 
-@_on_device
 def mnmt_pages_write(pool, layer, table, lens, k, v, start=None, max_q=None, stream=None):
     """Writes the codes k, v int8 [n, n_kv_heads * d_head] of new tokens, the last ones of their rows, into a layer's
     pages; row r has the tokens start[r] .. start[r + 1] - 1 (None: n / rows each), at most max_q as far as known."""
+    if _torch is None:
+        _with_torch()
     rows, width = table.shape
     shape, cfg, _ = _pool(pool, width, rows)
     at = pool.get_device()
@@ -455,7 +451,8 @@ def mnmt_pages_write(pool, layer, table, lens, k, v, start=None, max_q=None, str
     _need(_codes("v", v, d, at) == ld and v.shape[0] == n, "k and v must have the same rows and row stride")
     if start is not None:
         _ints("start", start, (rows + 1,), at)
-    _device(pool)
+    if at < 0 or at != _current():
+        return _elsewhere(at, mnmt_pages_write, pool, layer, table, lens, k, v, start, max_q, stream)
     rc = _lib.mnmt_pages_write(cfg, pool.data_ptr(), layer, table.data_ptr(), lens.data_ptr(), rows, k.data_ptr(),
                                v.data_ptr(), ld, _ptr(start), n, n if max_q is None else max_q, _stream(stream))
     if rc:
@@ -477,12 +474,13 @@ def _most(n, rows, start, max_q):
     return n // max(rows, 1) if start is None else n if max_q is None or max_q > n else max_q
 
 
-@_on_device
 def mnmt_attn_paged(q, pool, layer, table, lens, c_qk, c_pv, kind=ATTN_F32, start=None, causal=True, max_q=None,
                     max_len=None, out=None, stream=None):
     """Attention of the rows' last tokens, q int8 [n, n_heads * d_head], over a layer's pages: fp32 or (ATTN_I8) int8 of
     q's shape.  Row r has the tokens start[r] .. start[r + 1] - 1 (None: n / rows each); max_q and max_len: the most of
     a row and the longest length, as far as known."""
+    if _torch is None:
+        _with_torch()
     rows, width = table.shape
     shape, cfg, _ = _pool(pool, width, rows)
     at = pool.get_device()
@@ -492,7 +490,8 @@ def mnmt_attn_paged(q, pool, layer, table, lens, c_qk, c_pv, kind=ATTN_F32, star
     ld = _codes("q", q, d, at)
     if start is not None:
         _ints("start", start, (rows + 1,), at)
-    _device(pool)
+    if at < 0 or at != _current():
+        return _elsewhere(at, mnmt_attn_paged, q, pool, layer, table, lens, c_qk, c_pv, kind, start, causal, max_q, max_len, out, stream)
     out, ldo = _attn_out(q, kind, out)
     longest = width * shape.page_size
     a, nbytes = _attn(rows, n, shape.n_kv_heads, shape.d_head, d, kind, 1 if causal else 0, ld, ldo,
@@ -505,11 +504,12 @@ def mnmt_attn_paged(q, pool, layer, table, lens, c_qk, c_pv, kind=ATTN_F32, star
     return out
 
 
-@_on_device
 def mnmt_attn_cross(q, k, v, lens, d_head, c_qk, c_pv, kind=ATTN_F32, start=None, max_q=None, out=None, stream=None):
     """Attention of q int8 [n, n_heads * d_head] to the keys and values int8 [rows, S, n_kv_heads * d_head] of each
     query's source sentence, lens[b] of them: fp32 or (ATTN_I8) int8 of q's shape.  Sentence b has the queries
     start[b] .. start[b + 1] - 1 (None: n / rows each), at most max_q as far as known."""
+    if _torch is None:
+        _with_torch()
     rows, S, width = k.shape
     n, d = q.shape
     at = q.get_device()
@@ -523,7 +523,8 @@ def mnmt_attn_cross(q, k, v, lens, d_head, c_qk, c_pv, kind=ATTN_F32, start=None
     ldq = _codes("q", q, d, at)
     if start is not None:
         _ints("start", start, (rows + 1,), at)
-    _device(q)
+    if at < 0 or at != _current():
+        return _elsewhere(at, mnmt_attn_cross, q, k, v, lens, d_head, c_qk, c_pv, kind, start, max_q, out, stream)
     out, ldo = _attn_out(q, kind, out)
     hkv = width // d_head
     a, nbytes = _attn(rows, n, hkv, d_head, d, kind, 0, ldq, ldo, _most(n, rows, start, max_q), S, c_qk, c_pv)

@@ -125,6 +125,7 @@ def test_attention_configurations(kw, text):
     (dict(out=None), "null"), (dict(pool=ODD), "aligned"), (dict(q=ODD), "aligned"), (dict(out=ODD), "aligned"),
     (dict(cfg=attn(max_len=1 << 20), pages=pages(max_pages=1 << 12), ws_bytes=16), "workspace"),
     (dict(cfg=attn(max_len=1 << 20), pages=pages(max_pages=1 << 12), ws=None), "workspace"),
+    (dict(n=1 << 30), "2^30"),
     (dict(rows=1 << 20, n=1 << 20, pages=pages(n_kv_heads=16), cfg=attn(n_heads=16, ld_q=1024, ld_out=1024)), "2^23"),
 ], ids=str)
 def test_paged_attention(kw, text):
@@ -141,7 +142,7 @@ def test_paged_attention(kw, text):
     (dict(batch=-16), "batch"), (dict(S=-1), "S must"), (dict(rows=-1), "rows"), (dict(n=3), "multiple"),
     (dict(k=None), "null"), (dict(v=None), "null"), (dict(lens=None), "null"), (dict(q=None), "null"),
     (dict(out=None), "null"), (dict(k=ODD), "aligned"), (dict(v=ODD), "aligned"), (dict(q=ODD), "aligned"),
-    (dict(out=ODD), "aligned"), (dict(rows=(1 << 21) + 1, n=0), "2^23"),
+    (dict(out=ODD), "aligned"), (dict(rows=(1 << 21) + 1, n=0), "2^23"), (dict(n=1 << 30), "2^30"),
 ], ids=str)
 def test_cross_attention(kw, text):
     a = dict(hkv=4, dh=64, k=PTR, v=PTR, ld=512, batch=5120, S=10, lens=PTR, rows=4, q=PTR, start=None, n=8, out=PTR,

@@ -170,6 +170,56 @@ def test_bounds_are_hints(gpu, hints):
     run_paged(gpu, 17, [9000], [1], 4, 2, 64, 16, hints=dict(max_len=hints["max_len"]))
 
 
+@pytest.mark.parametrize("dh", [16, 32, 48, 64, 80, 96, 112, 128])
+@pytest.mark.parametrize("causal", [True, False])
+def test_large_chunks_over_head_widths(gpu, dh, causal):
+    """Chunks large enough for the kernels that share the keys between a block's queries; also with pages missing."""
+    def edit(table):
+        table[0, 3], table[0, 9], table[1, 20] = -1, 1 << 20, -3
+    run_paged(gpu, dh, [700, 611], [320, 201], 16, 2, dh, 32, causal=causal, table_edit=edit)
+
+
+@pytest.mark.parametrize("dh", [64, 128])
+@pytest.mark.parametrize("hints", [{}, dict(max_q=130), dict(max_q=130, max_len=600), dict(max_len=1500)])
+def test_large_chunks_over_long_rows(gpu, dh, hints):
+    """Few blocks and many keys: the keys in ranges, joined; rows beyond max_q and max_len too."""
+    run_paged(gpu, 40, [2600, 1333, 900], [300, 37, 150], 16, 2, dh, 16, hints=hints)
+
+
+def test_large_chunks_with_empty_rows(gpu):
+    got = run_paged(gpu, 41, [0, 100, 900, 1300], [70, 180, 300, 0], 16, 2, 64, 64, "i8", c_pv=9.0)
+    assert not got[:150].any() and got[150:].any()
+
+
+@pytest.mark.parametrize("dh", [16, 128])
+@pytest.mark.parametrize("paged", [True, False])
+def test_chunk_over_more_keys_than_one_fold(gpu, dh, paged):
+    """Integer sums hold 65,536 keys: 70,001 of them, some of the 4,100 queries compared."""
+    torch, mnmt = gpu
+    rng = np.random.default_rng(42)
+    n, S, P, hkv = 4100, 70001, 256, 2
+    q, some = codes(rng, n, hkv * dh), np.sort(rng.choice(n, 16, replace=False))
+    if paged:
+        pool, table = make(rng, 1, 280, hkv, P, dh, [S])
+        got = mnmt.mnmt_attn_paged(dev(torch, q), dev(torch, pool), 0, dev(torch, table), dev(torch, [S], np.int32), 1e-5, 1.0)
+        k, v, _ = R.Cache(pool).row(0, table[0], S)
+        seen = np.arange(S)[None, :] <= (S - n + some)[:, None]
+    else:
+        kv = codes(rng, 2, 1, S, hkv * dh)
+        got = mnmt.mnmt_attn_cross(dev(torch, q), dev(torch, kv[0]), dev(torch, kv[1]), dev(torch, [S], np.int32), dh, 1e-5, 1.0)
+        k, v = kv.reshape(2, S, hkv, dh)
+        seen = np.ones((16, S), bool)
+    ref, tol = R.attend(q[some].reshape(16, hkv, dh), k, v, seen, np.float32(1e-5), 1.0)
+    assert (np.abs(got.cpu().numpy()[some].reshape(ref.shape) - ref) <= tol).all()
+    assert np.linalg.norm(got.cpu().numpy()[some].reshape(ref.shape) - ref) <= 1e-5 * np.linalg.norm(ref)
+
+
+def test_many_rows_of_several_steps(gpu):
+    rng = np.random.default_rng(43)
+    run_paged(gpu, 43, rng.integers(1, 300, 270), [1] * 270, 8, 8, 64, 32)
+    run_paged(gpu, 44, rng.integers(1, 300, 530), [1] * 530, 8, 4, 128, 16, "i8", c_pv=6.0)
+
+
 def test_layers_and_dense_queries(gpu):
     run_paged(gpu, 18, [50, 20], [3, 3], 4, 4, 64, 16, layers=3, layer=2, strided=False)
 
@@ -290,6 +340,21 @@ def test_cross_lengths(gpu, S):
 
 def test_cross_chunk(gpu):
     run_cross(gpu, 30, [400, 333, 90], [150, 200, 1], 8, 8, 64, 400, hints=dict(max_q=5))
+
+
+@pytest.mark.parametrize("dh", [16, 32, 48, 64, 80, 96, 112, 128])
+def test_large_cross_chunks_over_head_widths(gpu, dh):
+    run_cross(gpu, dh, [600, 0, 333], [320, 50, 201], 16, 2, dh, 600, form=["pair", "apart", "late"][dh // 16 % 3])
+
+
+def test_large_cross_chunks_over_long_sources(gpu):
+    run_cross(gpu, 45, [2600, 1333], [300, 150], 16, 2, 64, 2600, "i8", c_pv=12.0, hints=dict(max_q=140))
+    run_cross(gpu, 46, [2600, 1333], [300, 150], 16, 2, 128, 2600)
+
+
+def test_cross_of_many_sentences(gpu):
+    rng = np.random.default_rng(47)
+    run_cross(gpu, 47, rng.integers(0, 200, 270), [4] * 270, 8, 8, 64, 200)
 
 
 def test_cross_no_source(gpu):
