@@ -797,19 +797,21 @@ __global__ __launch_bounds__(64 * kChunkWaves, 2) void k_attn_chunk(AttnArgs a) 
   }
 }
 
-// Joins the key ranges of a query tile; one block per query: a thread takes four
-// columns of every kParts-th range, eight of them at once, and the threads of a
-// column then join theirs.  The ranges are read before it is known how many there
-// are (what lies behind the last is not used).
-template <int NB>
+// Joins the key ranges of a query tile.  A thread takes four columns of a query;
+// where there are many ranges, kParts threads take every kParts-th of them, eight
+// at once, and the first of them then joins theirs.
+constexpr int kManySplits = 8;
+
+template <int NB, bool MANY>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
   constexpr int dh = 16 * NB, kPart = 16 * (dh + 2), U = 8;
-  constexpr int kCols = dh / 4, kParts = 256 / kCols < 16 ? 256 / kCols : 16;
-  __shared__ float4 ys[kParts][kCols];
-  __shared__ float tops[kParts], sums[kParts];
+  constexpr int kCols = dh / 4, kParts = !MANY ? 1 : 256 / kCols < 16 ? 256 / kCols : 16;
+  constexpr int kQueries = 256 / (kCols * kParts) < 16 ? 256 / (kCols * kParts) : 16;  // of a block at once
+  __shared__ float4 ys[MANY ? 256 : 1];
+  __shared__ float tops[MANY ? 256 : 1], sums[MANY ? 256 : 1];
   const int per_row = a.n_kv_heads * a.tiles;
   const int row = blockIdx.x / per_row, head = blockIdx.x % per_row / a.tiles;
-  const int mine = threadIdx.x / kCols, col = threadIdx.x % kCols;
+  const int slot = threadIdx.x / (kCols * kParts), mine = threadIdx.x / kCols % kParts, col = threadIdx.x % kCols;
   const AttnRow w = attn_row(a, row);
   for (int tile = blockIdx.x % a.tiles; 16 * tile < w.n * a.group; tile += a.tiles) {
     // a chunk's ranges go by its block's last tile
@@ -817,7 +819,10 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
     const int live = live_splits(a, tile_keys(a, w, min(tile / span * span + span - 1, last)));
     if (live == 1) continue;
     const float* part = a.part + tile_slot(a, w, row, head, tile, 0) * kPart;
-    for (int q = blockIdx.y; q < min(16, w.n * a.group - 16 * tile); q += gridDim.y) {
+    const int queries = min(16, w.n * a.group - 16 * tile);
+    for (int q0 = blockIdx.y * kQueries; q0 < queries; q0 += gridDim.y * kQueries) {
+      const int q = q0 + slot;
+      const bool active = slot < kQueries && q < queries;
       float top = (float)kNoReference, sum = 0.f;
       float4 y = make_float4(0.f, 0.f, 0.f, 0.f);
       auto join = [&](float ref, float s, float4 x) {
@@ -828,13 +833,14 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
         y = make_float4(fmaf(y.x, old, x.x * now), fmaf(y.y, old, x.y * now), fmaf(y.z, old, x.z * now),
                         fmaf(y.w, old, x.w * now));
       };
-      if (mine < kParts) {
+      if (active) {
         for (int s0 = mine; s0 < live; s0 += U * kParts) {
           float s[U], ref[U];
           float4 x[U];
 #pragma unroll
           for (int u = 0; u < U; ++u) {
-            const float* src = part + (size_t)min(s0 + u * kParts, a.splits - 1) * kPart;
+            if (s0 + u * kParts >= a.splits) break;
+            const float* src = part + (size_t)(s0 + u * kParts) * kPart;
             s[u] = src[16 * dh + q];
             ref[u] = src[16 * dh + 16 + q];
             x[u] = *(const float4*)(src + q * dh + 4 * col);
@@ -843,19 +849,20 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
           for (int u = 0; u < U; ++u)
             if (s0 + u * kParts < live) join(ref[u], s[u], x[u]);
         }
-        ys[mine][col] = y;
-        if (col == 0) {
-          tops[mine] = top;
-          sums[mine] = sum;
-        }
       }
-      __syncthreads();
-      if (mine == 0) {
+      if constexpr (MANY) {
+        ys[threadIdx.x] = y;
+        tops[threadIdx.x] = top;
+        sums[threadIdx.x] = sum;
+        __syncthreads();
+        if (active && mine == 0) {
 #pragma unroll
-        for (int p = 1; p < kParts; ++p) join(tops[p], sums[p], ys[p][col]);
-        store_joined(a, w, head, 16 * tile + q, 4 * col, dh, y, sum);
+          for (int p = 1; p < kParts; ++p)
+            join(tops[threadIdx.x + p * kCols], sums[threadIdx.x + p * kCols], ys[threadIdx.x + p * kCols]);
+        }
+        __syncthreads();
       }
-      __syncthreads();
+      if (active && mine == 0) store_joined(a, w, head, 16 * tile + q, 4 * col, dh, y, sum);
     }
   }
 }
@@ -877,8 +884,10 @@ hipError_t launch_attn_nb(const AttnArgs& a, hipStream_t s) {
     hipLaunchKernelGGL((k_attn<NB, PAGED, 1, false>), dim3((units + 3) / 4), dim3(256), 0, s, a);
   else
     hipLaunchKernelGGL((k_attn<NB, PAGED, 4, false>), dim3(units), dim3(256), 0, s, a);
-  if (a.splits > 1)
-    hipLaunchKernelGGL((k_attn_join<NB>), dim3(tiles, a.queries), dim3(256), 0, s, a);
+  if (a.splits > kManySplits)
+    hipLaunchKernelGGL((k_attn_join<NB, true>), dim3(tiles, a.queries), dim3(256), 0, s, a);
+  else if (a.splits > 1)
+    hipLaunchKernelGGL((k_attn_join<NB, false>), dim3(tiles), dim3(256), 0, s, a);
   return hipGetLastError();
 }
 

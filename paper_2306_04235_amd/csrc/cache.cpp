@@ -90,6 +90,20 @@ int run_attn(AttnArgs& a, bool paged, int d_head, int max_q, int max_len, void* 
 
 }  // namespace
 
+// A unit: a query tile (16 queries) of a row and key head.  Measured us, one form |
+// the other:
+// - The chunk kernels (waves 0) read keys and values once for a block's queries
+//   but are two launches with barriers: from eight tiles per head and enough work
+//   on.  Heads of 64: 4096 units x 700 keys 38 | 54, 1024 x 8000 87 | 109, 2048 x
+//   700 27 | 26, 512 x 1500 37 | 29.  Heads of 128: 2048 x 700 33 | 44, 1024 x 8000
+//   135 | 189, 1024 x 1000 35 | 32, 2048 x 200 21 | 20; of four tiles 2048 x 1000 72 | 50.
+// - One wave per unit from 512 units on (heads of 64, against four: 1024 x 700 18 | 59,
+//   512 x 1500 31 | 49, 256 x 1500 28 | 21), four below.
+// - The keys of a unit go to several waves or blocks, and are joined, while that
+//   fills the GPU twice over (16 rows of 8 key heads, 1000-32000 keys, 2048 blocks 117,
+//   1024 138, 4096 125), in ranges of at least 512 keys for four waves and 1024 for one.
+// - Rows of at most two steps (short) want waves more than keys a step ahead: 512
+//   rows of 8 heads, 20-80 keys, 10.4 | 12.3.
 AttnPlan plan_attn(int rows, int n, int n_kv_heads, int group, int d_head, int max_q, int max_len) {
   AttnPlan p{};
   const long heads = (long)rows * n_kv_heads;  // <= kMaxAttnUnits
@@ -99,23 +113,25 @@ AttnPlan plan_attn(int rows, int n, int n_kv_heads, int group, int d_head, int m
   p.queries = (int)std::max(1L, std::min(16L, (long)max_q * group));
   p.splits = 1;
   p.chunk = 1 << 30;
+  // `want` ranges of at least `least` keys
+  auto split = [&](long want, int least) {
+    want = std::min(want, (long)max_len / least);
+    if (want < 2) return;
+    p.chunk = (int)((max_len + want - 1) / want + 255) / 256 * 256;
+    p.splits = (max_len + p.chunk - 1) / p.chunk;
+  };
   p.is_short = max_len <= 128;
-  p.waves = p.is_short || units >= 2048 ? 1 : 4;
-  if (p.tiles >= 16 && max_len >= 512 && units >= 512) {
+  if (p.tiles >= 8 && units * max_len >= (d_head <= 64 ? 2800000L : 1000000L)) {
     p.waves = 0;
     p.tiles = (p.tiles + 7) / 8 * 8;
     const long blocks = heads * p.tiles / (d_head <= 64 ? 8 : 4);
-    const long want = std::min((512 + blocks - 1) / blocks, (long)(max_len + 1023) / 1024);
-    if (want > 1) {
-      p.chunk = (int)((max_len + want - 1) / want + 255) / 256 * 256;
-      p.splits = (max_len + p.chunk - 1) / p.chunk;
-    }
-  } else if (p.waves == 4 && max_len > 512 && units < 2048) {
-    const long want = std::min((2048 + units - 1) / units, (long)(max_len + 511) / 512);
-    if (want > 1) {
-      p.chunk = (int)((max_len + want - 1) / want + 255) / 256 * 256;
-      p.splits = (max_len + p.chunk - 1) / p.chunk;
-    }
+    split((512 + blocks - 1) / blocks, 1024);
+  } else if (p.is_short || units >= 512) {
+    p.waves = 1;
+    split((4096 + units - 1) / units, 1024);
+  } else {
+    p.waves = 4;
+    split((2048 + units - 1) / units, 512);
   }
   const size_t slots = ((size_t)n * group / 16 + rows + 1) * n_kv_heads * p.splits;  // tile_slot
   if (p.splits > 1) p.part_bytes = slots * 16 * (d_head + 2) * sizeof(float);

@@ -176,18 +176,18 @@ def test_large_chunks_over_head_widths(gpu, dh, causal):
     """Chunks large enough for the kernels that share the keys between a block's queries; also with pages missing."""
     def edit(table):
         table[0, 3], table[0, 9], table[1, 20] = -1, 1 << 20, -3
-    run_paged(gpu, dh, [700, 611], [320, 201], 16, 2, dh, 32, causal=causal, table_edit=edit)
+    run_paged(gpu, dh, [700, 611], [320, 201], 16, 2, dh, 32, causal=causal, table_edit=edit, width=200)  # (6400 keys at most)
 
 
 @pytest.mark.parametrize("dh", [64, 128])
-@pytest.mark.parametrize("hints", [{}, dict(max_q=130), dict(max_q=130, max_len=600), dict(max_len=1500)])
+@pytest.mark.parametrize("hints", [{}, dict(max_q=130), dict(max_q=290, max_len=1700), dict(max_len=2000)])
 def test_large_chunks_over_long_rows(gpu, dh, hints):
     """Few blocks and many keys: the keys in ranges, joined; rows beyond max_q and max_len too."""
-    run_paged(gpu, 40, [2600, 1333, 900], [300, 37, 150], 16, 2, dh, 16, hints=hints)
+    run_paged(gpu, 40, [2600, 1333, 900], [300, 37, 150], 16, 2, dh, 16, hints=hints, width=500)  # (8000 keys at most)
 
 
 def test_large_chunks_with_empty_rows(gpu):
-    got = run_paged(gpu, 41, [0, 100, 900, 1300], [70, 180, 300, 0], 16, 2, 64, 64, "i8", c_pv=9.0)
+    got = run_paged(gpu, 41, [0, 100, 900, 1300], [70, 180, 300, 0], 16, 2, 64, 64, "i8", c_pv=9.0, width=90)
     assert not got[:150].any() and got[150:].any()
 
 
@@ -344,12 +344,12 @@ def test_cross_chunk(gpu):
 
 @pytest.mark.parametrize("dh", [16, 32, 48, 64, 80, 96, 112, 128])
 def test_large_cross_chunks_over_head_widths(gpu, dh):
-    run_cross(gpu, dh, [600, 0, 333], [320, 50, 201], 16, 2, dh, 600, form=["pair", "apart", "late"][dh // 16 % 3])
+    run_cross(gpu, dh, [600, 0, 333], [320, 50, 201], 16, 2, dh, 4000, form=["pair", "apart", "late"][dh // 16 % 3])
 
 
 def test_large_cross_chunks_over_long_sources(gpu):
-    run_cross(gpu, 45, [2600, 1333], [300, 150], 16, 2, 64, 2600, "i8", c_pv=12.0, hints=dict(max_q=140))
-    run_cross(gpu, 46, [2600, 1333], [300, 150], 16, 2, 128, 2600)
+    run_cross(gpu, 45, [2600, 1333], [300, 150], 16, 2, 64, 5000, "i8", c_pv=12.0)
+    run_cross(gpu, 46, [2600, 1333], [300, 150], 16, 2, 128, 5000, hints=dict(max_q=140))
 
 
 def test_cross_of_many_sentences(gpu):
