@@ -91,6 +91,19 @@ __device__ __forceinline__ size_t tile_slot(const AttnArgs& a, const AttnRow& w,
   return (slot * a.n_kv_heads + head) * a.splits + split;
 }
 
+// The k-th row in the order in which blocks take them: the longest first, where
+// there are few (a wave compares them), so that no long one is left to the end.
+__device__ __forceinline__ int row_in_turn(const AttnArgs& a, int k) {
+  if (a.rows > 64) return k;
+  const int lane = threadIdx.x & 63, len = lane < a.rows ? attn_clamp(a.len[lane], 0, a.cap) : -1;
+  int longer = 0;
+  for (int r = 0; r < a.rows; ++r) {
+    const int other = __builtin_amdgcn_readlane(len, r);
+    longer += other > len || (other == len && r < lane);
+  }
+  return __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)__ballot(lane < a.rows && longer == k)) - 1);
+}
+
 // Where a lane finds its keys and values: pages, values [token / 16][dh][16].
 template <int NB>
 struct PagedKeys {
@@ -474,7 +487,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_top(AttnArgs a) {
   __shared__ int tops[4 * kTopTiles * 16];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4;
   const int groups = a.tiles / kTopTiles, per_head = groups * a.splits, per_row = per_head * a.n_kv_heads;
-  const int row = blockIdx.x / per_row, head = blockIdx.x % per_row / per_head;
+  const int row = row_in_turn(a, blockIdx.x / per_row), head = blockIdx.x % per_row / per_head;
   const int split = blockIdx.x % per_head / groups, group0 = groups - 1 - blockIdx.x % groups;
   const AttnRow w = attn_row(a, row);
   const int tiles = (w.n * a.group + 15) / 16;
@@ -611,7 +624,7 @@ __global__ __launch_bounds__(64 * kChunkWaves, 2) void k_attn_chunk(AttnArgs a) 
   // blocks of one row and head side by side, so that the L2s hold what they read,
   // the last tiles first (in a causal chunk they see most)
   const int groups = a.tiles / kTiles, per_head = groups * a.splits, per_row = per_head * a.n_kv_heads;
-  const int row = blockIdx.x / per_row, head = blockIdx.x % per_row / per_head;
+  const int row = row_in_turn(a, blockIdx.x / per_row), head = blockIdx.x % per_row / per_head;
   const int split = blockIdx.x % per_head / groups, group0 = groups - 1 - blockIdx.x % groups;
   const AttnRow w = attn_row(a, row);
   const int tiles = (w.n * a.group + 15) / 16;
