@@ -364,7 +364,10 @@ typedef struct {
 } mnmt_pages_cfg;
 
 /* Bytes of the pool, and of the workspace of a fork or compaction of `rows`
- * output rows; 0 where the arguments are refused.  Host only. */
+ * output rows; 0 where the arguments are refused.  Host only.  A workspace, here
+ * and below, needs no filling and keeps nothing between calls, but belongs to one
+ * call until its work is done: calls that may overlap (other streams, other
+ * captured graphs) need workspaces of their own. */
 size_t mnmt_pages_bytes(const mnmt_pages_cfg* cfg);
 size_t mnmt_pages_ws_bytes(const mnmt_pages_cfg* cfg, int rows);
 

@@ -33,7 +33,7 @@ namespace mnmt {
 
 constexpr int kAttnKeys = 64;         // keys per step of a wave
 constexpr int kNoReference = -(1 << 22);  // below every score (|s| <= 127^2 128 < 2^21)
-constexpr int kFoldSteps = 1024;      // steps after which the int32 sums are folded: 65536 * 2^14 < 2^31
+constexpr int kFoldSteps = 1024;      // steps that a chunk's int32 sums hold: 65536 keys * 2^14 < 2^31
 constexpr float kOne = 8355711.f;     // the fixed-point 1: 0x7F7F7F, the largest number with digits in range
 constexpr float kDigits = 8388608.f + 32896.f;
 constexpr uint32_t kDigitBits = 0x4B008080u;  // its bits: p = 0
@@ -284,7 +284,12 @@ struct TileSums {
 // One query tile per wave (WK 1) or per block, whose four waves take turns at
 // the keys (WK 4).  For few queries per row: every wave loads its keys and
 // values straight into the matrix operands.  SHORT: rows of one or two steps, where
-// more waves at once are worth more than keys a step ahead.
+// more waves at once are worth more than keys a step ahead.  Long rows are bound by
+// HBM (16 rows, 32 heads on 8 key heads of 128, 2824-30176 keys: 541 MB in 110 us,
+// 4.9 TB/s, of 5.2 that a read reaches), short ones by the latencies of length,
+// page, keys and store one after the other (512 rows of 8 heads of 64, 20-80 keys:
+// 10 us for 27 MB).  Folding the sums in every step is free in the first and takes
+// no registers between steps; the integer sums would need 96 for heads of 128.
 template <int NB, bool PAGED, int WK, bool SHORT>
 __global__ __launch_bounds__(256, !SHORT ? 2 : NB <= 4 ? 4 : 3) void k_attn(AttnArgs a) {
   constexpr int dh = 16 * NB, KS = (NB + 3) / 4;  // 64-wide slices of the head
@@ -596,7 +601,10 @@ __global__ __launch_bounds__(256, 2) void k_attn_top(AttnArgs a) {
 // slowest.)
 //
 // The references are the scores' maxima, from k_attn_top: they never move, so that
-// the sums are integers throughout and no step branches.
+// the sums are integers throughout and no step branches.  Bound by the vector unit
+// and the matrix cores, which overlap in part: per 16 queries and 64 keys of a head
+// of 128, 32 products of 16 cycles beside 150 instructions of 4 (exponentials 16,
+// digits 36), 1300-1600 cycles in all.
 constexpr int chunk_tiles(int nb) { return nb <= 4 ? 2 : 1; }  // of a wave
 constexpr int kChunkWaves = 4;
 constexpr int kValueGap = 16;  // between values' operands: the transposing stores meet no bank conflicts

@@ -251,7 +251,8 @@ __global__ __launch_bounds__(1024) void k_compact_plan(PagesFork f, const int* f
   compact_plan(f, [&](int p) { return *(const int4*)(first + p); }, to, list, info);
 }
 
-// Small caches: marks and plan in one launch, the marks in LDS.
+// Small caches: marks and plan in one launch, the marks in LDS (512 rows of 6
+// entries 6.6 us, bound by the chain parent - length - entry - list).
 constexpr int kSmallPages = 12288, kSmallEntries = 32768;
 
 template <bool COMPACT>
@@ -276,7 +277,7 @@ __global__ __launch_bounds__(1024) void k_pages_small(PagesFork f, int* place, i
 }
 
 // The rows' new table and, block row y > 0, their copied pages: one chunk of a
-// page of one layer.
+// page of one layer (47 MB of copies in 10.5 us).
 constexpr int kCopyBytes = 16384;
 
 __device__ __forceinline__ void copy_chunk(const PagesShape& s, int8_t* pool, int from, int to, int part) {
@@ -346,7 +347,8 @@ __global__ __launch_bounds__(256) void k_compact_apply(PagesFork f, const int* t
 }
 
 // Codes of new tokens into their pages: one block per group of 16 tokens and
-// row.  Values lie [dh][16] within a group, so a block that has the whole group
+// row.  Bound by HBM for chunks (82 MB in 22 us, 16 at a copy's rate: the loads all
+// come first, then the stores), by latencies for steps (512 tokens 4.6 us).  Values lie [dh][16] within a group, so a block that has the whole group
 // transposes dwords of 16 tokens in registers and stores 64 bytes per thread;
 // one that has part of it stores bytes.
 __global__ __launch_bounds__(256) void k_pages_write(PagesWrite w) {

@@ -158,8 +158,8 @@ def test_long_chunk_over_few_rows(gpu):
     run_paged(gpu, 14, [2000, 1024], [40, 24], 4, 2, 64, 32)
 
 
-def test_more_keys_than_one_fold(gpu):
-    """A wave folds its integer sums after 65,536 keys: one query tile over 140,000, with weights that hardly differ."""
+def test_many_keys_in_one_wave(gpu):
+    """One query tile over 140,000 keys in one wave, with weights that hardly differ."""
     run_paged(gpu, 15, [140000], [1], 1, 1, 16, 256, c_qk=1e-5, hints=dict(max_len=100))
 
 
@@ -580,9 +580,9 @@ def step_of(gpu, seed, rows=6, length=700):
     rng = np.random.default_rng(seed)
     h, dh, P = 4, 64, 16
     lens = np.full(rows, length)
-    pool, table = make(rng, 2, 60 * rows, h, P, dh, lens, width=60)
+    pool, table = make(rng, 2, 60 * rows, h, P, dh, lens, width=1000)  # (room for 16,000 keys: workspaces are needed)
     pd, td, ld = dev(torch, pool), dev(torch, table), dev(torch, lens, np.int32)
-    qkv = dev(torch, codes(rng, rows, 3 * h * dh))
+    qkv, q = dev(torch, codes(rng, rows, 3 * h * dh)), dev(torch, codes(rng, 130 * rows, h * dh))
     kv = dev(torch, codes(rng, rows, 600, 2 * h * dh))
     slen = dev(torch, rng.integers(1, 600, rows), np.int32)
     parent, one = dev(torch, rng.integers(0, rows, rows), np.int32), torch.ones(rows, dtype=torch.int32, device="cuda")
@@ -592,8 +592,9 @@ def step_of(gpu, seed, rows=6, length=700):
         t, l, info = mnmt.mnmt_pages_fork(pd, td, ld, parent=parent, new=one, stream=stream)
         mnmt.mnmt_pages_write(pd, 1, t, l, qkv[:, d: 2 * d], qkv[:, 2 * d:], stream=stream)
         a = mnmt.mnmt_attn_paged(qkv[:, :d], pd, 1, t, l, 1e-4, 0.5, stream=stream)
+        c = mnmt.mnmt_attn_paged(q, pd, 1, t, l, 1e-4, 0.5, stream=stream)  # the last 130 tokens once more
         x = mnmt.mnmt_attn_cross(qkv[:, :d], kv[..., :d], kv[..., d:], slen, dh, 1e-4, 0.5, stream=stream)
-        return t, l, info, a, x
+        return t, l, info, a, c, x
 
     return step, qkv, pd
 
