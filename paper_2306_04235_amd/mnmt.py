@@ -316,8 +316,10 @@ def _pages(pool_shape, width: int, rows: int):
 
 @functools.lru_cache(maxsize=256)
 def _attn(rows, n, hkv, dh, d, kind, causal, ld, ldo, most, longest, c_qk, c_pv):
-    """An attention call's configuration and workspace."""
+    """An attention call's configuration and workspace.  (Plain numbers all: a tensor would be known by its identity.)"""
     _need(dh > 0 and d > 0 and d % dh == 0, "q must have whole heads")
+    # (ctypes would take such a number's low bits)
+    _need(max(rows, n, d, ld, ldo, most, longest) < 1 << 31, "sizes and strides must be below 2^31")
     a = AttnCfg(d // dh, kind, causal, ld, ldo, most, longest, c_qk, c_pv)
     return C.byref(a), lib().mnmt_attn_ws_bytes(rows, n, d // dh, hkv, dh, most, longest)
 
@@ -348,12 +350,9 @@ def _codes(name, t, width, device):
     return stride if n > 1 else w
 
 
-def _workspace(nbytes, like, stream):
+def _workspace(nbytes, like):
     """A call's own workspace, so that calls on different streams and captured graphs never share one."""
-    t = _torch.empty(nbytes, dtype=_torch.uint8, device=like.device)
-    if stream is not None:
-        t.record_stream(stream)  # (the allocator would give it to the current stream's next call)
-    return t
+    return _torch.empty(nbytes, dtype=_torch.uint8, device=like.device)
 
 
 _torch = _int8 = _int32 = _current = None
@@ -369,10 +368,12 @@ def _with_torch():
     _torch = torch
 
 
-def _elsewhere(device, call, *args):
-    """The call with the tensors' device as the current one: its launches and its stream belong there."""
+def _elsewhere(device, stream, call, *args):
+    """The call with the tensors' device and a given stream as the current ones.  Its launches belong there, and so do its
+    workspace and new outputs: memory of another stream's may still be in use by that stream's work."""
     _need(device >= 0, "the tensors must be on a GPU")
-    with _torch.cuda.device(device):
+    _need(stream is None or stream.device_index == device, "the stream must be of the tensors' device")
+    with _torch.cuda.device(device), _torch.cuda.stream(stream):
         return call(*args)
 
 
@@ -392,8 +393,8 @@ def mnmt_pages_fork(pool, table, lens, parent=None, new=None, out=None, stream=N
         _ints("parent", parent, (rows,), at)
     if new is not None:
         _ints("new", new, (rows,), at)
-    if at < 0 or at != _current():
-        return _elsewhere(at, mnmt_pages_fork, pool, table, lens, parent, new, out, stream)
+    if stream is not None or at < 0 or at != _current():
+        return _elsewhere(at, stream, mnmt_pages_fork, pool, table, lens, parent, new, out)
     if out is None:
         # one allocation: the lengths and the counts lie behind the table
         flat = _torch.empty(rows * (width + 1) + 2, dtype=_int32, device=pool.device)
@@ -401,10 +402,10 @@ def mnmt_pages_fork(pool, table, lens, parent=None, new=None, out=None, stream=N
     else:
         for name, t, shape in zip(("out[0]", "out[1]", "out[2]"), out, ((rows, width), (rows,), (2,))):
             _ints(name, t, shape, at)
-    ws = _workspace(nbytes, pool, stream)
+    ws = _workspace(nbytes, pool)
     rc = _lib.mnmt_pages_fork(cfg, pool.data_ptr(), table.data_ptr(), lens.data_ptr(), rows_in, _ptr(parent), _ptr(new),
                               rows, out[0].data_ptr(), out[1].data_ptr(), out[2].data_ptr(), ws.data_ptr(), nbytes,
-                              _stream(stream))
+                              _stream())
     if rc:
         _check(rc, "mnmt_pages_fork")
     return out
@@ -420,17 +421,17 @@ def mnmt_pages_compact(pool, table, lens, out=None, stream=None):
     at = pool.get_device()
     _ints("table", table, (rows, width), at)
     _ints("lens", lens, (rows,), at)
-    if at < 0 or at != _current():
-        return _elsewhere(at, mnmt_pages_compact, pool, table, lens, out, stream)
+    if stream is not None or at < 0 or at != _current():
+        return _elsewhere(at, stream, mnmt_pages_compact, pool, table, lens, out)
     if out is None:
         flat = _torch.empty(rows * width + 2, dtype=_int32, device=pool.device)
         out = (flat[:-2].view(rows, width), flat[-2:])
     else:
         _ints("out[0]", out[0], (rows, width), at)
         _ints("out[1]", out[1], (2,), at)
-    ws = _workspace(nbytes, pool, stream)
+    ws = _workspace(nbytes, pool)
     rc = _lib.mnmt_pages_compact(cfg, pool.data_ptr(), table.data_ptr(), lens.data_ptr(), rows, out[0].data_ptr(),
-                                 out[1].data_ptr(), ws.data_ptr(), nbytes, _stream(stream))
+                                 out[1].data_ptr(), ws.data_ptr(), nbytes, _stream())
     if rc:
         _check(rc, "mnmt_pages_compact")
     return out
@@ -449,12 +450,13 @@ def mnmt_pages_write(pool, layer, table, lens, k, v, start=None, max_q=None, str
     d = shape.n_kv_heads * shape.d_head
     ld, n = _codes("k", k, d, at), k.shape[0]
     _need(_codes("v", v, d, at) == ld and v.shape[0] == n, "k and v must have the same rows and row stride")
+    _need(n < 1 << 31, "there must be fewer than 2^31 tokens")
     if start is not None:
         _ints("start", start, (rows + 1,), at)
-    if at < 0 or at != _current():
-        return _elsewhere(at, mnmt_pages_write, pool, layer, table, lens, k, v, start, max_q, stream)
+    if stream is not None or at < 0 or at != _current():
+        return _elsewhere(at, stream, mnmt_pages_write, pool, layer, table, lens, k, v, start, max_q)
     rc = _lib.mnmt_pages_write(cfg, pool.data_ptr(), layer, table.data_ptr(), lens.data_ptr(), rows, k.data_ptr(),
-                               v.data_ptr(), ld, _ptr(start), n, n if max_q is None else max_q, _stream(stream))
+                               v.data_ptr(), ld, _ptr(start), n, n if max_q is None else min(int(max_q), n), _stream())
     if rc:
         _check(rc, "mnmt_pages_write")
 
@@ -471,7 +473,7 @@ def _attn_out(q, kind, out):
 
 def _most(n, rows, start, max_q):
     """The most queries of a row, as far as known."""
-    return n // max(rows, 1) if start is None else n if max_q is None or max_q > n else max_q
+    return n // max(rows, 1) if start is None else n if max_q is None or max_q > n else int(max_q)
 
 
 def mnmt_attn_paged(q, pool, layer, table, lens, c_qk, c_pv, kind=ATTN_F32, start=None, causal=True, max_q=None,
@@ -490,15 +492,17 @@ def mnmt_attn_paged(q, pool, layer, table, lens, c_qk, c_pv, kind=ATTN_F32, star
     ld = _codes("q", q, d, at)
     if start is not None:
         _ints("start", start, (rows + 1,), at)
-    if at < 0 or at != _current():
-        return _elsewhere(at, mnmt_attn_paged, q, pool, layer, table, lens, c_qk, c_pv, kind, start, causal, max_q, max_len, out, stream)
+    if stream is not None or at < 0 or at != _current():
+        return _elsewhere(at, stream, mnmt_attn_paged, q, pool, layer, table, lens, c_qk, c_pv, kind, start, causal, max_q,
+                          max_len, out)
     out, ldo = _attn_out(q, kind, out)
     longest = width * shape.page_size
     a, nbytes = _attn(rows, n, shape.n_kv_heads, shape.d_head, d, kind, 1 if causal else 0, ld, ldo,
-                      _most(n, rows, start, max_q), longest if max_len is None else min(max_len, longest), c_qk, c_pv)
-    ws = _workspace(nbytes, q, stream) if nbytes else None
+                      _most(n, rows, start, max_q), longest if max_len is None else min(int(max_len), longest),
+                      float(c_qk), float(c_pv))
+    ws = _workspace(nbytes, q) if nbytes else None
     rc = _lib.mnmt_attn_paged(cfg, a, pool.data_ptr(), layer, table.data_ptr(), lens.data_ptr(), rows, q.data_ptr(),
-                              _ptr(start), n, out.data_ptr(), _ptr(ws), nbytes, _stream(stream))
+                              _ptr(start), n, out.data_ptr(), _ptr(ws), nbytes, _stream())
     if rc:
         _check(rc, "mnmt_attn_paged")
     return out
@@ -523,15 +527,16 @@ def mnmt_attn_cross(q, k, v, lens, d_head, c_qk, c_pv, kind=ATTN_F32, start=None
     ldq = _codes("q", q, d, at)
     if start is not None:
         _ints("start", start, (rows + 1,), at)
-    if at < 0 or at != _current():
-        return _elsewhere(at, mnmt_attn_cross, q, k, v, lens, d_head, c_qk, c_pv, kind, start, max_q, out, stream)
+    if stream is not None or at < 0 or at != _current():
+        return _elsewhere(at, stream, mnmt_attn_cross, q, k, v, lens, d_head, c_qk, c_pv, kind, start, max_q, out)
     out, ldo = _attn_out(q, kind, out)
     hkv = width // d_head
-    a, nbytes = _attn(rows, n, hkv, d_head, d, kind, 0, ldq, ldo, _most(n, rows, start, max_q), S, c_qk, c_pv)
-    ws = _workspace(nbytes, q, stream) if nbytes else None
+    a, nbytes = _attn(rows, n, hkv, d_head, d, kind, 0, ldq, ldo, _most(n, rows, start, max_q), S, float(c_qk),
+                      float(c_pv))
+    ws = _workspace(nbytes, q) if nbytes else None
     rc = _lib.mnmt_attn_cross(a, hkv, d_head, k.data_ptr(), v.data_ptr(), ld if S > 1 else width, batch if rows > 1 else 0,
                               S, lens.data_ptr(), rows, q.data_ptr(), _ptr(start), n, out.data_ptr(), _ptr(ws), nbytes,
-                              _stream(stream))
+                              _stream())
     if rc:
         _check(rc, "mnmt_attn_cross")
     return out

@@ -182,3 +182,12 @@ def test_binding_refuses_what_the_kernels_would_misread():
                 lambda: mnmt.mnmt_pages_compact(pool, table, lens[:1])):
         with pytest.raises(ValueError):
             bad()
+
+
+@pytest.mark.parametrize("at", [0, 1, 4, 7, 8, 9, 10])
+def test_binding_refuses_numbers_past_32_bits(at):
+    args = [1, 1, 1, 16, 16, mnmt.ATTN_F32, 1, 16, 16, 1, 1, 1.0, 1.0]
+    mnmt._attn(*args)
+    args[at] += 1 << 32
+    with pytest.raises(ValueError):
+        mnmt._attn(*args)
