@@ -381,10 +381,11 @@ size_t mnmt_pages_ws_bytes(const mnmt_pages_cfg* cfg, int rows);
  * if no row shares it, the others get copies, of all layers.  Copies and new
  * pages are taken from the free pages in ascending order, by the rows in
  * order.  Pages that only dropped rows had are free.
- * d_info int32 [2]: free pages left, pages missing.  Where pages are missing
- * (or a length would exceed the table: it stops there) the entries that got none
- * are -1, and nothing has been copied: the input tables still hold, and the call
- * can be made again with fewer rows.
+ * A length that would exceed the table stops at its capacity.
+ * d_info int32 [2]: free pages left, pages missing.  Where pages are missing the
+ * entries that got none are -1, and nothing has been copied: the input tables (if
+ * they are not the output's) still hold, and the call can be made again with
+ * fewer rows.
  * The outputs may not overlap the inputs, except that without d_parent they may
  * be the input table and lengths themselves. */
 int mnmt_pages_fork(const mnmt_pages_cfg* cfg, void* d_pool, const int32_t* d_table, const int32_t* d_len, int rows_in,

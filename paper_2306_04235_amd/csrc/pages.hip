@@ -222,7 +222,9 @@ __device__ __forceinline__ void plan_free(const PagesFork& f, At4 at4, int* plac
   if (threadIdx.x == 0) place[f.rows] = n;
 }
 
-// to[p]: where page p goes, -1 where it is free (one block).
+// to[p]: where page p goes, -1 where it is free; list: the free pages below the
+// live pages' count, and from its middle on the pages that move there (one block).
+// (As many move as there are free ones below: at most half of all.)
 template <class At4>
 __device__ __forceinline__ void compact_plan(const PagesFork& f, At4 at4, int* to, int* list, int32_t* info) {
   const int n = f.s.n_pages;
@@ -232,7 +234,10 @@ __device__ __forceinline__ void compact_plan(const PagesFork& f, At4 at4, int* t
   const int live = block_list(0, n, at4, used, [&](int p, int) { to[p] = p; });
   block_list(0, live, at4, [](int x) { return x == kFree; }, [&](int p, int k) { list[k] = p; });
   __syncthreads();
-  const int moved = block_list(live, n, at4, used, [&](int p, int k) { to[p] = list[k]; });
+  const int moved = block_list(live, n, at4, used, [&](int p, int k) {
+    to[p] = list[k];
+    list[n / 2 + k] = p;
+  });
   if (threadIdx.x == 0) {
     info[0] = live;
     info[1] = moved;
@@ -276,8 +281,7 @@ __global__ __launch_bounds__(1024) void k_pages_small(PagesFork f, int* place, i
   }
 }
 
-// The rows' new table and, block row y > 0, their copied pages: one chunk of a
-// page of one layer (47 MB of copies in 10.5 us).
+// One chunk of a page of one layer (47 MB of copies in 10.5 us).
 constexpr int kCopyBytes = 16384;
 
 __device__ __forceinline__ void copy_chunk(const PagesShape& s, int8_t* pool, int from, int to, int part) {
@@ -296,12 +300,14 @@ __device__ __forceinline__ void copy_chunk(const PagesShape& s, int8_t* pool, in
     if (threadIdx.x + 256 * i < n) dst[threadIdx.x + 256 * i] = x[i];
 }
 
-__global__ __launch_bounds__(256) void k_fork_apply(PagesFork f, const int* place, const int* source, const int* list,
+// The rows' new table and, block row y > 0, their copied pages, chunk after chunk.
+__global__ __launch_bounds__(256) void k_fork_apply(PagesFork f, int parts, const int* place, const int* source, const int* list,
                                                     int32_t* table_out, int32_t* len_out, int32_t* info) {
   const int r = blockIdx.x, src = r < f.rows ? source[r] : -1, free_pages = place[f.rows], want = place[f.rows + 1];
   const int at = r < f.rows ? place[r] : 0;
   if (blockIdx.y > 0) {  // nothing is copied where pages are missing: the input tables still hold
-    if (src >= 0 && want <= free_pages) copy_chunk(f.s, f.pool, src, list[at], blockIdx.y - 1);
+    if (src < 0 || want > free_pages) return;
+    for (int part = blockIdx.y - 1; part < parts; part += gridDim.y - 1) copy_chunk(f.s, f.pool, src, list[at], part);
     return;
   }
   if (r == 0 && threadIdx.x == 0) {
@@ -325,19 +331,19 @@ __global__ __launch_bounds__(256) void k_fork_apply(PagesFork f, const int* plac
   }
 }
 
-// Block row 0: the table's new numbers, a row per block; the others: one chunk of
-// a page of one layer, a page per block.
-__global__ __launch_bounds__(256) void k_compact_apply(PagesFork f, const int* to, const int32_t* info,
-                                                       int32_t* table_out) {
-  if (blockIdx.y > 0) {
-    // only the pages from info[0] on move
-    const int p = blockIdx.x + info[0];
-    if (p >= f.s.n_pages) return;
-    const int q = to[p];
-    if (q >= 0) copy_chunk(f.s, f.pool, p, q, blockIdx.y - 1);
+// The table's new numbers, a row to each of the first blocks; the others go over
+// the chunks of the pages that move.
+__global__ __launch_bounds__(256) void k_compact_apply(PagesFork f, int tables, int parts, const int* to,
+                                                       const int* list, const int32_t* info, int32_t* table_out) {
+  if ((int)blockIdx.x >= tables) {
+    const int moved = info[1], *from = list + f.s.n_pages / 2;
+    for (long i = blockIdx.x - tables; i < (long)moved * parts; i += gridDim.x - tables) {
+      const int k = (int)(i / parts);
+      copy_chunk(f.s, f.pool, from[k], list[k], (int)(i - (long)k * parts));
+    }
     return;
   }
-  for (int r = blockIdx.x; r < f.rows; r += gridDim.x) {
+  for (int r = blockIdx.x; r < f.rows; r += tables) {
     const int n = plan_row(f, r).old;
     for (int c = threadIdx.x; c < f.s.max_pages; c += 256) {
       const int page = c < n ? page_at(f.s, f.table, r, c) : -1;
@@ -364,17 +370,16 @@ __global__ __launch_bounds__(256) void k_pages_write(PagesWrite w) {
   }
   if (n <= 0) return;
   const long cap = (long)w.s.max_pages << w.s.shift;
-  const int len = max(w.len[r], 0), begin = max(len - n, 0);
-  const int end = (int)min((long)len, cap);  // (past the table's capacity there is nothing to write to)
+  const int len = clamped(w.len[r], 0, cap), begin = max(len - n, 0);
   const long off = (long)len - n - a;        // position of token t: t + off
   const int D = w.s.n_kv_heads * w.s.d_head, dh = w.s.d_head;
   const size_t vhalf = w.s.page_bytes / 2;
-  for (int g = begin / 16 + blockIdx.y; g * 16L < end; g += gridDim.y) {
+  for (int g = begin / 16 + blockIdx.y; 16 * g < len; g += gridDim.y) {
     const int page = page_at(w.s, w.table, r, g >> (w.s.shift - 4));
     if (page < 0) continue;
     int8_t* kp = w.pool + (size_t)page * w.s.page_bytes;
     int8_t* vp = kp + vhalf;
-    const int lo = max(begin - 16 * g, 0), hi = min(end - 16 * g, 16), g_in = g & ((w.s.page_size >> 4) - 1);
+    const int lo = max(begin - 16 * g, 0), hi = min(len - 16 * g, 16), g_in = g & ((w.s.page_size >> 4) - 1);
     const long t0 = 16L * g - off;  // token at the group's first place (before the first new one where lo > 0)
     const int cpr = D / 16;
     auto key_to = [&](int i) {  // chunk i of the new keys' 16-byte chunks
@@ -443,6 +448,11 @@ PagesWs split_ws(const PagesShape& s, int rows, void* ws) {
   return w;
 }
 
+// Blocks that copy: not one to each chunk that there might be, most of which no
+// call copies (compaction of 8192 pages of 32 layers and 256 KB, nothing to move: 453
+// us with a block to each, 15 without).
+constexpr int kCopyBlocks = 65536, kMoveBlocks = 8192;
+
 int clear_blocks(int n) { return std::min((n + 1023) / 1024, 1024); }
 
 }  // namespace
@@ -477,8 +487,10 @@ hipError_t launch_pages_fork(const PagesFork& f, int32_t* table_out, int32_t* le
     mark_pages(f, w.first, s);
     hipLaunchKernelGGL(k_fork_plan, dim3(2), dim3(1024), 0, s, f, w.first, w.place, w.source, w.list);
   }
-  hipLaunchKernelGGL(k_fork_apply, dim3(std::max(f.rows, 1), 1 + pages_copy_parts(f.s)), dim3(256), 0, s, f, w.place,
-                     w.source, w.list, table_out, len_out, info);
+  const int parts = pages_copy_parts(f.s), rows = std::max(f.rows, 1);
+  const int blocks = std::min(parts, std::max(1, kCopyBlocks / rows));  // of a row
+  hipLaunchKernelGGL(k_fork_apply, dim3(rows, 1 + blocks), dim3(256), 0, s, f, parts, w.place, w.source, w.list,
+                     table_out, len_out, info);
   return hipGetLastError();
 }
 
@@ -491,9 +503,12 @@ hipError_t launch_pages_compact(const PagesFork& f, int32_t* table_out, int32_t*
     mark_pages(f, w.first, s);
     hipLaunchKernelGGL(k_compact_plan, dim3(1), dim3(1024), 0, s, f, w.first, to, w.list, info);
   }
-  if (f.rows > 0)
-    hipLaunchKernelGGL(k_compact_apply, dim3(f.s.n_pages, 1 + pages_copy_parts(f.s)), dim3(256), 0, s, f, to, info,
+  if (f.rows > 0) {
+    const int parts = pages_copy_parts(f.s), tables = std::min(f.rows, 1024);
+    const int copies = (int)std::min((long)(f.s.n_pages / 2) * parts, (long)kMoveBlocks);
+    hipLaunchKernelGGL(k_compact_apply, dim3(tables + copies), dim3(256), 0, s, f, tables, parts, to, w.list, info,
                        table_out);
+  }
   return hipGetLastError();
 }
 

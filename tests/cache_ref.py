@@ -81,9 +81,10 @@ class Cache:
     def write(self, layer, table, lens, k, v, start):
         for r in range(len(lens)):
             a, b = int(start[r]), int(start[r + 1])
+            length = min(max(int(lens[r]), 0), table.shape[1] * self.P)
             for i in range(a, b):
-                t = int(lens[r]) - (b - a) + (i - a)
-                if 0 <= t < table.shape[1] * self.P and self.there(int(table[r, t // self.P])):
+                t = length - (b - a) + (i - a)
+                if t >= 0 and self.there(int(table[r, t // self.P])):
                     self.k[layer, table[r, t // self.P], :, t % self.P] = k[i].reshape(self.hkv, self.dh)
                     self.v[layer, table[r, t // self.P], :, t % self.P] = v[i].reshape(self.hkv, self.dh)
 

@@ -1,6 +1,8 @@
 """The paged cache and the attention operators on the GPU against the plain
 forms of cache_ref.py: whole numbers exactly, attention within a derived bound
 of float64."""
+import types
+
 import numpy as np
 import pytest
 
@@ -227,6 +229,19 @@ def test_layers_and_dense_queries(gpu):
 def test_many_rows(gpu):
     rng = np.random.default_rng(19)
     run_paged(gpu, 19, rng.integers(1, 100, 700), [1] * 700, 8, 8, 64, 16)
+
+
+def test_scales_changed_in_place(gpu):
+    """Scales given as tensors count as they are at each call."""
+    torch, mnmt = gpu
+    rng = np.random.default_rng(15)
+    pool, table = make(rng, 1, 4, 1, 16, 16, [30])
+    args = dev(torch, codes(rng, 1, 16)), dev(torch, pool), 0, dev(torch, table), dev(torch, np.array([30]), np.int32)
+    c_qk, c_pv = torch.tensor(1e-3), torch.tensor(0.5)
+    mnmt.mnmt_attn_paged(*args, c_qk, c_pv)
+    c_qk *= 4
+    c_pv *= 3
+    assert torch.equal(mnmt.mnmt_attn_paged(*args, c_qk, c_pv), mnmt.mnmt_attn_paged(*args, float(c_qk), float(c_pv)))
 
 
 def test_tokens_of_no_row_are_left(gpu):
@@ -468,6 +483,29 @@ def test_compact_random(gpu, seed):
         assert np.array_equal(p.cpu().numpy(), ref.pool())
 
 
+@pytest.mark.parametrize("L, n_pages, hkv, P, dh", [(2, 600, 8, 64, 64), (3, 17001, 2, 16, 32), (1, 1, 1, 16, 16)])
+def test_compact_and_fork_of_many_parts(gpu, L, n_pages, hkv, P, dh):
+    """More chunks to copy than there are blocks for them."""
+    torch, mnmt = gpu
+    rng = np.random.default_rng(n_pages)
+    count = max(n_pages // 2 // 8, 1)
+    lens = np.full(count, min(8, n_pages) * P - 1)
+    pool, table = make(rng, L, n_pages, hkv, P, dh, lens)
+    p = dev(torch, pool)
+    got = mnmt.mnmt_pages_compact(p, dev(torch, table), dev(torch, lens, np.int32))
+    ref = R.Cache(pool)
+    want = ref.compact(table, lens)
+    assert np.array_equal(got[0].cpu().numpy(), want[0]) and np.array_equal(got[1].cpu().numpy(), want[1])
+    assert np.array_equal(p.cpu().numpy(), ref.pool())
+
+
+def test_fork_of_many_rows_and_chunks(gpu):
+    """More chunks to copy than a row has blocks for them."""
+    rng = np.random.default_rng(10)
+    pool, table = make(rng, 9, 9100, 2, 16, 16, np.full(40, 20))
+    forked(gpu, pool, table, np.full(40, 20), rng.integers(0, 40, 9000), np.ones(9000, int))
+
+
 @pytest.mark.parametrize("P, hkv, dh", [(16, 4, 64), (32, 1, 16), (64, 3, 80), (256, 2, 128)])
 @pytest.mark.parametrize("ragged", [True, False])
 def test_write(gpu, P, hkv, dh, ragged):
@@ -490,6 +528,20 @@ def test_write(gpu, P, hkv, dh, ragged):
         ref.write(1, table, lens, both[:, hkv * dh: 2 * hkv * dh], both[:, 2 * hkv * dh:], start)
         assert np.array_equal(pd.cpu().numpy(), ref.pool())
         pd.copy_(dev(torch, pool))
+
+
+def test_write_lengths_out_of_range(gpu):
+    """Lengths below zero and past the table count as the nearest in range, as for attention."""
+    torch, mnmt = gpu
+    rng = np.random.default_rng(9)
+    lens = np.array([-4, 1 << 30, 70, (1 << 31) - 1, -(1 << 31)])
+    new = np.array([3, 20, 70, 5, 1])
+    pool, table = make(rng, 1, 30, 2, 16, 32, [64, 64, 64, 64, 64], width=4)
+    pd, kd = dev(torch, pool), dev(torch, codes(rng, 99, 64))
+    mnmt.mnmt_pages_write(pd, 0, dev(torch, table), dev(torch, lens, np.int32), kd, kd, start=dev(torch, starts(new), np.int32))
+    ref = R.Cache(pool)
+    ref.write(0, table, lens, kd.cpu().numpy(), kd.cpu().numpy(), starts(new))
+    assert np.array_equal(pd.cpu().numpy(), ref.pool())
 
 
 # ---- together --------------------------------------------------------------------------
@@ -651,3 +703,38 @@ def test_streams(gpu):
     for outs, w in zip(got, want):
         for o in outs:
             assert all(torch.equal(a, b) for a, b in zip(o, w))
+
+
+def test_memory_of_a_given_streams_call(gpu):
+    """A call on a given stream takes no memory that the current stream freed but may still use."""
+    torch, _ = gpu
+    step, _, _ = step_of(gpu, 80, rows=3, length=900)
+    want = [x.clone() for x in step()]
+    side = torch.cuda.Stream()
+    for stream in (side, None):  # (both allocators' blocks are there)
+        step(stream=stream)
+    torch.cuda.synchronize()
+    torch.cuda.empty_cache()
+    junk = [torch.empty(1 << n, dtype=torch.uint8, device="cuda") for n in range(9, 27) for _ in range(4)]
+    for _ in range(40):
+        for x in junk:
+            x.fill_(77)
+    del junk, x
+    got = step(stream=side)
+    torch.cuda.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+
+
+def test_stream_of_another_device(gpu):
+    torch, mnmt = gpu
+    pool = torch.zeros((1, 2, 2, 1, 16, 16), dtype=torch.int8, device="cuda")
+    table, lens = torch.zeros((1, 1), dtype=torch.int32, device="cuda"), torch.ones(1, dtype=torch.int32, device="cuda")
+    q = torch.zeros((1, 16), dtype=torch.int8, device="cuda")
+    other = types.SimpleNamespace(device_index=1, cuda_stream=0)
+    for call in (lambda: mnmt.mnmt_pages_fork(pool, table, lens, stream=other),
+                 lambda: mnmt.mnmt_pages_compact(pool, table, lens, stream=other),
+                 lambda: mnmt.mnmt_pages_write(pool, 0, table, lens, q, q, stream=other),
+                 lambda: mnmt.mnmt_attn_paged(q, pool, 0, table, lens, 1.0, 1.0, stream=other),
+                 lambda: mnmt.mnmt_attn_cross(q, q[None], q[None], lens, 16, 1.0, 1.0, stream=other)):
+        with pytest.raises(ValueError, match="stream"):
+            call()
