@@ -20,7 +20,7 @@
 // softmax is fp32 throughout in effect, and the sums do not depend on order.
 //
 // Scores are taken relative to the largest so far (steps) or of all (chunks), an
-// int32 that starts the products' accumulators at its negative for nothing.
+// int32 that the products' accumulators start below for nothing.
 #pragma once
 
 #include <climits>
@@ -37,6 +37,10 @@ constexpr int kFoldSteps = 1024;      // steps that a chunk's int32 sums hold: 6
 constexpr float kOne = 8355711.f;     // the fixed-point 1: 0x7F7F7F, the largest number with digits in range
 constexpr float kDigits = 8388608.f + 32896.f;
 constexpr uint32_t kDigitBits = 0x4B008080u;  // its bits: p = 0
+// The bits of 2^24.  Taken as a float, kScore + d is 2^24 + d for -2^23 <= d <= 0:
+// scores' accumulators start there, and need no conversion (a chunk of 301-2048
+// tokens over up to 8191 keys 311 -> 302 us).
+constexpr int kScore = 0x4B800000;
 
 __device__ __forceinline__ int attn_clamp(int v, int lo, int hi) { return v < lo ? lo : v > hi ? hi : v; }
 
@@ -198,12 +202,13 @@ __device__ __forceinline__ int largest(v4i (&d)[4], bool masked, int count) {
   return top;
 }
 
-// Exponents c2 d, and -inf in the place of those of masked keys.
+// Exponents c2 d of kScore + d (one rounding: 2^24 c2 is exact), and -inf in the
+// place of those of masked keys.
 __device__ __forceinline__ void exponents(const v4i (&d)[4], float c2, float (&x)[4][4]) {
 #pragma unroll
   for (int j = 0; j < 4; ++j)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) x[j][i] = (float)d[j][i] * c2;
+    for (int i = 0; i < 4; ++i) x[j][i] = fmaf(__int_as_float(d[j][i]), c2, -16777216.f * c2);
 }
 __device__ __forceinline__ void hide(int count, float (&x)[4][4]) {
 #pragma unroll
@@ -371,7 +376,7 @@ __global__ __launch_bounds__(256, !SHORT ? 2 : NB <= 4 ? 4 : 3) void k_attn(Attn
       v4i d[4], p[3];
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
-        d[j] = mfma16(kf[j][0], t.q[0], v4i{-y.ref, -y.ref, -y.ref, -y.ref});
+        d[j] = mfma16(kf[j][0], t.q[0], v4i{kScore - y.ref, kScore - y.ref, kScore - y.ref, kScore - y.ref});
 #pragma unroll
         for (int s = 1; s < KS; ++s) d[j] = mfma16(kf[j][s], t.q[s], d[j]);
       }
@@ -380,7 +385,7 @@ __global__ __launch_bounds__(256, !SHORT ? 2 : NB <= 4 ? 4 : 3) void k_attn(Attn
       if (!SHORT && more) load_keys(key + kAttnKeys * WK);
       const bool masked = key + kAttnKeys > all_see || __any(!there);
       const int count = there ? min(t.mine, kend) - key - 16 * g : 0;
-      const int up = max(quad_max(largest(d, masked, count)), 0);
+      const int up = max(quad_max(largest(d, masked, count)) - kScore, 0);
       const float scale = __builtin_amdgcn_exp2f(-(float)up * a.c2);
 #pragma unroll
       for (int j = 0; j < 4; ++j)
@@ -603,7 +608,7 @@ __global__ __launch_bounds__(256, 2) void k_attn_top(AttnArgs a) {
 // The references are the scores' maxima, from k_attn_top: they never move, so that
 // the sums are integers throughout and no step branches.  Bound by the vector unit
 // and the matrix cores, which overlap in part: per 16 queries and 64 keys of a head
-// of 128, 32 products of 16 cycles beside 150 instructions of 4 (exponentials 16,
+// of 128, 32 products of 16 cycles beside 134 instructions of 4 (exponentials 16,
 // digits 36), 1300-1600 cycles in all.
 constexpr int chunk_tiles(int nb) { return nb <= 4 ? 2 : 1; }  // of a wave
 constexpr int kChunkWaves = 4;
@@ -700,7 +705,7 @@ __global__ __launch_bounds__(64 * kChunkWaves, 2) void k_attn_chunk(AttnArgs a) 
     auto look = [&](int key) {
       if constexpr (PAGED) at.look(min(key, kend - 1));
     };
-    auto scores = [&](const int8_t* buf, v4i (&d)[QT][4], const int (&ref)[QT]) {
+    auto scores = [&](const int8_t* buf, v4i (&d)[QT][4], const int (&from)[QT]) {
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         v4i k[KS];
@@ -708,7 +713,7 @@ __global__ __launch_bounds__(64 * kChunkWaves, 2) void k_attn_chunk(AttnArgs a) 
         for (int s = 0; s < KS; ++s) k[s] = *(const v4i*)(buf + (j * KS + s) * 1024 + 16 * lane);
 #pragma unroll
         for (int x = 0; x < QT; ++x) {
-          d[x][j] = mfma16(k[0], t[x].q[0], v4i{-ref[x], -ref[x], -ref[x], -ref[x]});
+          d[x][j] = mfma16(k[0], t[x].q[0], v4i{from[x], from[x], from[x], from[x]});
 #pragma unroll
           for (int s = 1; s < KS; ++s) d[x][j] = mfma16(k[s], t[x].q[s], d[x][j]);
         }
@@ -716,11 +721,13 @@ __global__ __launch_bounds__(64 * kChunkWaves, 2) void k_attn_chunk(AttnArgs a) 
     };
     __syncthreads();  // (the last group's reads of LDS are over)
     if (kbegin < kend) {
-      int ref[QT], cur = 0;
+      int from[QT], cur = 0;
 #pragma unroll
-      for (int x = 0; x < QT; ++x)
-        ref[x] = y[x].ref =
+      for (int x = 0; x < QT; ++x) {
+        y[x].ref =
             tile + x < tiles ? a.tops[tile_slot(a, w, row, head, tile + x, split) * 16 + (lane & 15)] : kNoReference;
+        from[x] = kScore - y[x].ref;
+      }
       // the weights of a step, and the products of the step before, which need
       // nothing of it: the matrix and the vector unit work side by side
       look(kbegin);
@@ -759,7 +766,7 @@ __global__ __launch_bounds__(64 * kChunkWaves, 2) void k_attn_chunk(AttnArgs a) 
           const bool more = key + kAttnKeys < kend;
           v4i d[QT][4], v[NB];
           float x[QT][4][4];
-          scores(kbuf + cur * kKeyBytes, d, ref);
+          scores(kbuf + cur * kKeyBytes, d, from);
           values(v);
           // nothing is read from LDS between here and the next step: a read would
           // wait for these loads
